@@ -418,6 +418,182 @@ int sprnn_transpose_csr(int rows, int cols, const int32_t* row_ptr, const int32_
 int sprnn_project(sprnn_handle_t h, int T, int input_size, const float* x_in, const uint16_t* w_in_fp16_bits,
                   const float* bias, float* b_prime, void* stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * The other operators of a layer on sequences [T][B][H]: a recurrence with a diagonal, input-dependent matrix
+ * (selective scan), the short convolution, the norm and the 8-bit projection that stand in front of one.
+ *
+ * They keep nothing between calls: no handle, every buffer is the caller's, and calls may run at the same time on
+ * different streams as long as they share no buffer that one of them writes (workspaces included).  All of them only
+ * enqueue work, allocate nothing, and may be captured in a HIP graph.  `device_id` is the GPU that holds the buffers.
+ * Parameters are float32; activations have the call's type; sums, states and norms are held in float32, and a result is
+ * rounded to its type once.  Outputs must not overlap inputs unless said otherwise.  Limits: T 0..2^22, B 0..65535, T * B
+ * below 2^31, channels (rows, widths) 1..2^24; offsets inside a buffer are 64 bits wide.
+ *
+ * lengths: device int32 [B] or NULL (every sample has T steps): sample b has the steps t < lengths[b] (values outside
+ * 0..T count as 0 or T).  Inputs behind a sample's end are not used, whatever they hold; outputs there are written as
+ * zeros, and the state that a call returns is the one behind the sample's last step.
+ */
+enum { SPRNN_TYPE_F32 = 0, SPRNN_TYPE_F16 = 1, SPRNN_TYPE_BF16 = 2, SPRNN_TYPE_E4M3 = 3 };
+
+/* A sequence [T][B][H] inside a device buffer: element (t, b, i) is data[t * step + b * sample + i], strides in elements
+ * (>= 0), so time-major, batch-major and a range of the channels of a wider tensor are all the same.  data must be aligned
+ * to its element.  Rows of an output must not overlap. */
+typedef struct sprnn_seq_s {
+  void* data;
+  int64_t step, sample;
+} sprnn_seq_t;
+
+/*
+ * Selective scan: C channels of N states each, the matrix of the recurrence diagonal and different in every step.
+ *   v_t = dt_t + dt_bias,   d_t = softplus(v_t) (or v_t itself),
+ *   h_t[c][n] = exp(d_t[c] A[c][n]) h_{t-1}[c][n] + d_t[c] u_t[c] B_t[g][n]        g = c / (C / groups)
+ *   y_t[c] = (sum_n C_t[g][n] h_t[c][n] + D[c] u_t[c]) * silu(z_t[c])
+ * d_t A is expected to be at most 0 (A negative, d_t positive), as such layers are.  C is at most 2^20 here, and two steps
+ * of a sequence are at most 2^25 elements apart.
+ */
+typedef struct sprnn_scan_s {
+  int steps, batch;            /* T, B                                                                  */
+  int channels, states;        /* C, N 1..128                                                           */
+  int groups;                  /* divides C: neighbouring channels share B_t and C_t                    */
+  int type;                    /* SPRNN_TYPE_F32, F16 or BF16: u, dt, z, B, C, y and their gradients    */
+  int softplus;                /* 1: d = softplus(v), 0: d = v                                          */
+  sprnn_seq_t u, dt;           /* [T][B][C]                                                             */
+  sprnn_seq_t z;               /* [T][B][C], or data NULL: no gate                                      */
+  sprnn_seq_t B, C;            /* [T][B][groups * N]: group g's states at g * N                         */
+  const float* A;              /* [C][N]                                                                */
+  const float* D;              /* [C] or NULL (zeros)                                                   */
+  const float* dt_bias;        /* [C] or NULL (zeros)                                                   */
+  const int32_t* lengths;      /* [B] or NULL                                                           */
+} sprnn_scan_t;
+
+/* Bytes of the buffers that the calls below need for these sizes (steps, batch, channels, states and groups are read):
+ * workspaces of the two passes and what the forward pass keeps for the backward pass.  Any pointer may be NULL. */
+int sprnn_scan_sizes(const sprnn_scan_t* scan, int64_t* forward_workspace, int64_t* backward_workspace, int64_t* kept);
+
+/*
+ *   state_in   [B][C][N] float32 or NULL (zeros): h_0.
+ *   y          [T][B][C].
+ *   state_out  [B][C][N] float32 or NULL: h behind the last step.  May be state_in itself: the next token of a running
+ *              sequence is a call of one step with its state in place.
+ *   kept       NULL, or a buffer of the size above that the backward pass reads.
+ *   workspace  buffer of at least the size above, 16-byte aligned like kept; its contents mean nothing between calls.
+ */
+int sprnn_scan_forward(int device_id, const sprnn_scan_t* scan, const float* state_in, sprnn_seq_t y, float* state_out,
+                       void* kept, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Gradients of a loss; a NULL output is not wanted.  Sums over samples, steps and channels have an order that depends on
+ * the sizes alone: the same call gives the same bits. */
+typedef struct sprnn_scan_gradients_s {
+  sprnn_seq_t u, dt, z;        /* [T][B][C]; data of z NULL without a gate                              */
+  sprnn_seq_t B, C;            /* [T][B][groups * N]                                                    */
+  float* A;                    /* [C][N]                                                                */
+  float* D;                    /* [C]                                                                   */
+  float* dt_bias;              /* [C]                                                                   */
+  float* state;                /* [B][C][N]: of state_in                                                */
+} sprnn_scan_gradients_t;
+
+/*
+ *   dy           [T][B][C]: gradient of y.
+ *   d_state_out  [B][C][N] float32 or NULL (zeros): gradient of state_out.
+ *   kept         what sprnn_scan_forward kept for the same scan.
+ */
+int sprnn_scan_backward(int device_id, const sprnn_scan_t* scan, sprnn_seq_t dy, const float* d_state_out, const void* kept,
+                        const sprnn_scan_gradients_t* gradients, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Causal depthwise convolution over a channel's last K inputs, the K - 1 before the call taken from a state:
+ *   p_t[c] = bias[c] + sum_k weight[c][k] x_{t-K+1+k}[c],    y_t[c] = p_t[c] sigmoid(p_t[c])  (silu = 1)  or  p_t[c].
+ * state: [K - 1][B][C] of the call's type, the K - 1 inputs before step 0 (oldest first; NULL: zeros), or the last K - 1
+ * inputs behind the call.
+ */
+typedef struct sprnn_conv_s {
+  int steps, batch, channels;  /* T, B, C                                                               */
+  int width;                   /* K 1..8                                                                */
+  int type;                    /* SPRNN_TYPE_F32, F16 or BF16                                           */
+  int silu;
+  sprnn_seq_t x;               /* [T][B][C]                                                             */
+  const float* weight;         /* [C][K]                                                                */
+  const float* bias;           /* [C] or NULL (zeros)                                                   */
+  const void* state;           /* [K - 1][B][C] or NULL (zeros)                                         */
+  const int32_t* lengths;      /* [B] or NULL                                                           */
+} sprnn_conv_t;
+
+/* state_out may be NULL, and may be the state itself (the next token of a running sequence: a call of one step). */
+int sprnn_conv_forward(int device_id, const sprnn_conv_t* conv, sprnn_seq_t y, void* state_out, void* stream);
+
+/* Bytes of the workspace of the backward pass (steps, batch, channels and width are read). */
+int sprnn_conv_sizes(const sprnn_conv_t* conv, int64_t* backward_workspace);
+
+/*
+ *   dy [T][B][C]; d_state_out [K - 1][B][C] of the call's type or NULL (zeros): gradient of state_out.
+ *   dx [T][B][C]; d_weight float32 [C][K], d_bias float32 [C], d_state [K - 1][B][C] of the call's type: each may be NULL.
+ * The same call gives the same bits.
+ */
+int sprnn_conv_backward(int device_id, const sprnn_conv_t* conv, sprnn_seq_t dy, const void* d_state_out, sprnn_seq_t dx,
+                        float* d_weight, float* d_bias, void* d_state, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Root-mean-square norm of the rows (t, b), after the addition of a residual stream:
+ *   r = x + residual  (rounded to the residual's type: the stream that goes on),   y = r / sqrt(mean_i r_i^2 + eps) * weight.
+ * Without a residual r is x.
+ */
+typedef struct sprnn_norm_s {
+  int steps, batch, width;     /* T, B, W                                                               */
+  int type;                    /* SPRNN_TYPE_F32, F16 or BF16: x, y                                     */
+  int residual_type;           /* type, or SPRNN_TYPE_F32: residual and residual_out                    */
+  float eps;                   /* >= 0                                                                  */
+  const float* weight;         /* [W] or NULL (ones)                                                    */
+} sprnn_norm_t;
+
+/*
+ *   residual, residual_out  data NULL: none (residual_out alone receives x).  residual_out may be residual itself.
+ *   y_type  type: y in the call's type, scales NULL.  SPRNN_TYPE_E4M3: every block of 128 of a row (the last one may be
+ *           shorter) gets the scale s = max(max |y|, 2^-100) / 448, y holds y / s as e4m3 (the finite-only format, no
+ *           infinities; 1 byte an element) and scales, float32 [T][B][ceil(W / 128)] contiguous, receives s.
+ *           A block that holds a NaN comes out as NaN.
+ */
+int sprnn_rms_norm(int device_id, const sprnn_norm_t* norm, sprnn_seq_t x, sprnn_seq_t residual, sprnn_seq_t residual_out,
+                   int y_type, sprnn_seq_t y, float* scales, void* stream);
+
+/* Bytes of the workspace of the backward pass (steps, batch and width are read). */
+int sprnn_rms_norm_sizes(const sprnn_norm_t* norm, int64_t* backward_workspace);
+
+/*
+ *   dy          [T][B][W], the call's type: gradient of y.
+ *   r           [T][B][W], the residual's type: the rows that were normed (residual_out, or x).
+ *   d_residual  [T][B][W], the residual's type, or data NULL (zeros): gradient of residual_out from elsewhere.
+ *   dr          [T][B][W], the residual's type: gradient of r, which is that of x and that of residual.
+ *   d_weight    float32 [W] or NULL.
+ * The same call gives the same bits.
+ */
+int sprnn_rms_norm_backward(int device_id, const sprnn_norm_t* norm, sprnn_seq_t dy, sprnn_seq_t r, sprnn_seq_t d_residual,
+                            sprnn_seq_t dr, float* d_weight, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * The input projection of sprnn_project with operands of 8 bits: rows of x in e4m3 with a scale per 128 (as sprnn_rms_norm
+ * writes them), weights in e4m3 with a scale per 128 x 128,
+ *   out[t][b][r] = sum_k (x[t][b][k] sx[t][b][k / 128]) (w[r][k] sw[r / 128][k / 128]) + bias[r].
+ * Products are exact and the sums of the scaled blocks are float32.  So are the sums over a block for float32 outputs; for
+ * outputs of 16 bits these come from the matrix instruction on e4m3, which adds eight neighbouring products with about 13
+ * bits (1.4e-5 of the result's norm over random inputs, a hundredth of its rounding to bfloat16, a tenth of that to float16).
+ *   steps, batch    T, B;  rows: R, outputs of a vector;  inputs: K.
+ *   x               e4m3 [T][B][K];  x_scales float32 [T][B][ceil(K / 128)] contiguous.
+ *   w               e4m3 [R][K] contiguous;  w_scales float32 [ceil(R / 128)][ceil(K / 128)] contiguous.
+ *   bias            float32 [R] or NULL.
+ *   out             [T][B][R] of out_type (SPRNN_TYPE_F32, F16, BF16).  float32 and contiguous it is the x of the forward
+ *                   calls above.
+ * The gradient of x is the same call with the gradient of out in 8 bits and w transposed.
+ */
+typedef struct sprnn_product_s {
+  int steps, batch, rows, inputs;
+  sprnn_seq_t x;
+  const float* x_scales;
+  const void* w;
+  const float* w_scales;
+  const float* bias;
+} sprnn_product_t;
+int sprnn_project_quantized(int device_id, const sprnn_product_t* product, int out_type, sprnn_seq_t out, void* stream);
+
 /*
  * Non-persistent comparison path: one kernel launch per timestep that re-reads the CSR weights
  * from device memory every step (the per-timestep sparse product the paper compares against in

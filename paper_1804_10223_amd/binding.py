@@ -36,7 +36,9 @@ EXPORTS = ["sprnn_create", "sprnn_create_ex", "sprnn_forward", "sprnn_forward_no
            "sprnn_backward_gru", "sprnn_backward_gru_with_weights",
            "sprnn_project", "sprnn_backward", "sprnn_backward_with_weights", "sprnn_weight_gradient", "sprnn_transpose_csr",
            "sprnn_get_info", "sprnn_read_timeline", "sprnn_check", "sprnn_pack_host", "sprnn_free_host", "sprnn_status_string",
-           "sprnn_destroy"]
+           "sprnn_destroy",
+           "sprnn_scan_sizes", "sprnn_scan_forward", "sprnn_scan_backward", "sprnn_conv_forward", "sprnn_conv_sizes", "sprnn_conv_backward",
+           "sprnn_rms_norm", "sprnn_rms_norm_sizes", "sprnn_rms_norm_backward", "sprnn_project_quantized"]   # argument types: see ops
 
 
 class Options(ctypes.Structure):

@@ -14,6 +14,7 @@
 #include "sprnn.h"
 #include "sprnn_contest.h"
 #include "sprnn_device.h"
+#include "sprnn_guard.h"
 #include "sprnn_pack.h"
 #include "sprnn_wgrad.h"
 
@@ -73,27 +74,6 @@ static unsigned char* g_scratch[kMaxScratchDevices];   // per device, null until
 static std::mutex g_scratch_mutex;
 
 namespace {
-
-// With SPRNN_DEBUG set in the environment, a failing HIP call is named on stderr.
-bool hip_ok(hipError_t e, const char* what) {
-  if (e == hipSuccess) return true;
-  static const bool verbose = std::getenv("SPRNN_DEBUG") != nullptr;
-  if (verbose) std::fprintf(stderr, "sprnn: %s failed: %s\n", what, hipGetErrorString(e));
-  (void)hipGetLastError();
-  return false;
-}
-#define SPRNN_HIP(call) hip_ok((call), #call)
-
-struct DeviceGuard {
-  int prev = -1;
-  bool ok = false;
-  explicit DeviceGuard(int dev) {
-    if (!SPRNN_HIP(hipGetDevice(&prev))) return;
-    ok = (prev == dev) || SPRNN_HIP(hipSetDevice(dev));
-    if (prev == dev) prev = -1;
-  }
-  ~DeviceGuard() { if (prev >= 0) (void)hipSetDevice(prev); }
-};
 
 void fill_info(const Mapping& m, int capacity, double pass_factor, sprnn_info_t* info) {
   std::memset(info, 0, sizeof(*info));

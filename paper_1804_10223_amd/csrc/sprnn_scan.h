@@ -1,0 +1,133 @@
+// Selective scan: what its forward and backward kernels share.
+//
+//   d_t = softplus(dt_t + dt_bias),  a_t = exp(d_t A),  h_t = a_t h_{t-1} + d_t u_t B_t,  y_t = (C_t h_t + D u_t) silu(z_t)
+//
+// A state costs one exponential and four multiply-adds a step, and the vector units set the pace: 16 cycles of a SIMD for
+// the exponential of a wavefront, 4 for each of the others.  So states live in registers, everything that depends on (step,
+// channel) alone is done once for all states of a channel, and steps are independent only through the state: where the
+// samples and channels are too few to fill the chip, time is divided into segments.  Segments but the last are run once from
+// a zero state for their effect (end state, sum of d: the product of all a of a state is exp(A sum d)), a small kernel
+// chains these, and a second run starts every segment from its true state.
+#ifndef SPRNN_SCAN_H_
+#define SPRNN_SCAN_H_
+
+#include "sprnn_seq.h"
+
+namespace sprnn {
+
+typedef float floatx4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kTile = 8;               // steps fetched together; the backward pass reads the state in front of every tile
+constexpr int kStatesMost = 128;
+constexpr int kSimds = 1024;           // of the chip: 256 CUs of four
+
+// How a scan is laid out: `quads` groups of four states (the last may be partial), states in memory of this library's own
+// [..][quad][C][4], so that neighbouring channels are neighbouring 16 bytes.
+struct ScanShape {
+  int T, B, C, N, G;
+  int per_group;                       // channels that share B and C
+  int quads;
+  int segments, segment;               // segments of time and their steps (a multiple of kTile)
+  int back_segments, back_segment;     // ... of the backward pass
+  int64_t state_floats() const { return (int64_t)B * quads * C * 4; }
+};
+ScanShape scan_shape(const sprnn_scan_t* p);
+
+struct ScanArgs {
+  int T, B, C, N, G, per_group, blocks, quads, softplus;   // blocks: wavefronts per group of channels
+  int segment;
+  const float* A;
+  const float* D;
+  const float* dt_bias;
+  const int32_t* lengths;
+};
+inline ScanArgs scan_arguments(const sprnn_scan_t* p, const ScanShape& s) {
+  return ScanArgs{s.T, s.B, s.C, s.N, s.G, s.per_group, 0, s.quads, p->softplus, s.segment, p->A, p->D, p->dt_bias, p->lengths};
+}
+bool good_scan(const sprnn_scan_t* p);
+
+// The rows t .. t + kTile - 1 of one sample as a buffer: an element is found by a 32-bit offset, loads of rows that are not
+// there give zeros and stores to them nothing, both without a branch.  (Rows of an input may lie closer than they are long;
+// then what is read of a row that is not there is some element of another: callers do not use it.)
+constexpr int64_t kStepMost = (int64_t)1 << 25;   // elements between two steps: eight rows stay below 2^31 bytes
+template <typename E>
+struct Tile {
+  __amdgpu_buffer_rsrc_t buffer;
+  uint32_t step;                       // bytes between rows
+  typedef typename std::remove_const<E>::type V;
+  __device__ __forceinline__ uint32_t offset(uint32_t row, uint32_t i) const { return row * step + i * (uint32_t)sizeof(E); }
+  __device__ __forceinline__ V load(uint32_t row, uint32_t i) const { return load_at(offset(row, i)); }
+  __device__ __forceinline__ void store(uint32_t row, uint32_t i, float f) const { store_at(offset(row, i), f); }
+  __device__ __forceinline__ V load_at(uint32_t byte) const {
+    const int at = (int)byte;
+    if constexpr (sizeof(E) == 4) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b32(buffer, at, 0, 0));
+    else return __builtin_bit_cast(V, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(buffer, at, 0, 0));
+  }
+  __device__ __forceinline__ void store_at(uint32_t byte, float f) const {
+    const int at = (int)byte;
+    const V v = (V)f;
+    if constexpr (sizeof(E) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), buffer, at, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), buffer, at, 0, 0);
+  }
+};
+// One sample's rows, tile by tile: all that a tile needs is an address, a stride and how many rows there are.
+template <typename E>
+struct Cursor {
+  uint64_t base;
+  uint32_t step;                       // bytes between rows
+  __device__ __forceinline__ Cursor(const View<E>& v, int t, int b, int offset = 0)
+      : base(reinterpret_cast<uint64_t>(v.data + ((int64_t)t * v.step + (int64_t)b * v.sample + offset))), step((uint32_t)v.step * (uint32_t)sizeof(E)) {}
+  // (width: elements of a row, 0 where there is no tensor)
+  __device__ __forceinline__ Tile<E> tile(int rows, int width) const {
+    rows = min(rows, kTile);
+    uint32_t own_step = step;            // offsets are formed where they are used: kept for every row of every tensor they
+    asm volatile("" : "+s"(own_step));   // would fill the registers that the states are in
+    const uint32_t bytes = width > 0 && rows > 0 ? (uint32_t)(rows - 1) * own_step + (uint32_t)width * (uint32_t)sizeof(E) : 0u;
+    const uint64_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)base), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(base >> 32));
+    return Tile<E>{__builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(lo | hi << 32), 0, __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000), own_step};
+  }
+  __device__ __forceinline__ void forth() { base += (uint64_t)kTile * step; }
+  __device__ __forceinline__ void back() { base -= (uint64_t)kTile * step; }
+};
+// One sample's states in this library's own layout, [quad][C][4]: an element's offset stays below 2^31 bytes.
+constexpr int kChannelsMost = 1 << 20;
+struct States {
+  __amdgpu_buffer_rsrc_t buffer;
+  int channels;
+  __device__ __forceinline__ States(const float* base, int64_t copy, int b, int batch, int quads, int channels) : channels(channels) {
+    const uint64_t at = reinterpret_cast<uint64_t>(base + (copy * batch + b) * quads * channels * 4);
+    const uint64_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32));
+    buffer = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(lo | hi << 32), 0, base ? quads * channels * 16 : 0, 0x00020000);
+  }
+  __device__ __forceinline__ floatx4_t load(int quad, int c) const {          // zeros behind the last quad
+    return __builtin_bit_cast(floatx4_t, __builtin_amdgcn_raw_buffer_load_b128(buffer, (quad * channels + c) * 16, 0, 0));
+  }
+  __device__ __forceinline__ void store(int quad, int c, const floatx4_t& v) const {
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(words, v), buffer, (quad * channels + c) * 16, 0, 0);
+  }
+};
+
+// d from v = dt + dt_bias.  exp(v) with the rounding of v log2(e) taken back, log1p by the rounding of 1 + e taken back:
+// both would otherwise cost the small steps (v far below 0) their last digits.
+__device__ __forceinline__ float softplus(float v) {
+  const float hi = v * kLog2e;
+  const float lo = __builtin_fmaf(v, kLog2e, -hi) + v * 1.925963033500e-08f;
+  float e = exp2_fast(hi);
+  e = __builtin_fmaf(e, lo * kLn2, e);
+  const float s = 1.0f + e, back = s - 1.0f;
+  const float log1p = __builtin_amdgcn_logf(s) * kLn2 * (e * __builtin_amdgcn_rcpf(back));
+  return v > 20.0f ? v : back == 0.0f ? e : log1p;
+}
+
+// The end states of segments 1.. (run from zero) chained into the true states in front of every segment:
+// H[0] = first, H[s + 1] += exp(A sums[s]) H[s].
+// (first: [B][C][N] as the callers have it, or null for zeros).
+hipError_t launch_chain(const ScanArgs& a, int segments, const float* first, float* H, const float* sums, hipStream_t stream);
+
+int64_t scan_backward_bytes(const ScanShape& s);
+hipError_t launch_scan_backward(const ScanShape& s, const sprnn_scan_t* p, const sprnn_seq_t& dy, const float* d_state_out, const float* kept,
+                                const sprnn_scan_gradients_t* out, float* workspace, hipStream_t stream);
+
+}  // namespace sprnn
+#endif

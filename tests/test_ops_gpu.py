@@ -1,0 +1,668 @@
+"""GPU tests of the operators in paper_1804_10223_amd.ops against their definitions in 64 bits (ops_oracle).
+
+Tolerances: the number of roundings on the longest path from an input to a result, times half a step of binary32, times the
+same sums over absolute values, plus the rounding of the result to its type (half a step).
+"""
+import numpy as np
+import pytest
+import torch
+
+import ops_oracle as ref
+from ops_oracle import EPS, half_step, smallest
+
+pytestmark = pytest.mark.gpu
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+TYPES = {"f32": F32, "f16": F16, "bf16": BF16}
+
+
+def _ops():
+    from paper_1804_10223_amd import ops
+    return ops
+
+
+def _close(got, want, scale, roundings, what, rows=None):
+    """|got - want| <= roundings * EPS * scale + the rounding to got's type; rows: relative errors further on."""
+    got = got.detach().cpu()
+    assert got.shape == want.shape, (what, got.shape, want.shape)
+    step = half_step(got.dtype) if got.dtype != F32 else EPS
+    bound = roundings * EPS * scale.abs() * (1.0 + step) + step * want.abs() + smallest(got.dtype)
+    off = (got.double() - want).abs()
+    assert torch.isfinite(got.double()).all(), what
+    worst = (off - bound).max() if off.numel() else torch.tensor(-1.0)
+    print("%s: %.3g of its bound" % (what, float((off / bound).max()) if off.numel() else 0.0), flush=True)
+    assert worst <= 0, (what, float(worst), float(off.max()))
+
+
+def _place(x, layout, fill=float("nan")):
+    """The CPU tensor x [T, B, ...] on the GPU: time-major, batch-major, or a range of a wider tensor at an odd offset."""
+    if x is None:
+        return None
+    if layout == "time":
+        return x.cuda()
+    if layout == "batch":
+        return x.transpose(0, 1).contiguous().cuda().transpose(0, 1)
+    T, B = x.shape[:2]
+    inner = int(np.prod(x.shape[2:]))
+    wide = torch.full((T, B, inner + 5), fill, dtype=x.dtype, device="cuda")
+    part = wide[:, :, 3:3 + inner]
+    part.copy_(x.reshape(T, B, inner))
+    return part.unflatten(2, x.shape[2:]) if x.dim() > 3 else part
+
+
+# ---------------------------------------------------------------------------------------------------------------- scan
+
+def _scan_case(T, B, C, N, G, dtype, gate, softplus, bias, D, state, lengths, seed):
+    gen = torch.Generator().manual_seed(seed)
+    normal = lambda *s: torch.randn(s, generator=gen)
+    low = lambda x: x.to(dtype)
+    case = dict(u=low(normal(T, B, C)), dt=low(normal(T, B, C) * 0.7 if softplus else torch.rand((T, B, C), generator=gen)),
+                A=-torch.rand((C, N), generator=gen) * 3 - 0.05, B=low(normal(T, B, G, N)), C=low(normal(T, B, G, N)),
+                D=normal(C) if D else None, z=low(normal(T, B, C)) if gate else None, dt_bias=normal(C) - 1.0 if bias else None,
+                state=normal(B, C, N) if state else None)
+    if lengths is not None:      # what lies behind a sample's end is not used, whatever it is
+        for k in ("u", "dt", "B", "C", "z"):
+            if case[k] is not None:
+                for i, n in enumerate(ref.ends_of(lengths, T, B)):
+                    case[k][n:, i] = float("nan") if i % 2 else float("inf")
+    return case
+
+
+def _double(case):
+    return {k: None if v is None else v.double() for k, v in case.items()}
+
+
+def _scan_roundings(T, N, C, case, softplus):
+    """One step multiplies the state by a (its argument d A has the relative error of d, 10, plus 3: times |d A|, plus 2 of
+    the exponential itself) and adds d u B (13): 2 + 13 |d A| + 16 for each of T steps, back and forth; then sums over
+    states, and in the gradients over channels, samples and steps."""
+    v = case["dt"].double()
+    v = v[torch.isfinite(v)]
+    most = float(v.max()) + (0.0 if case["dt_bias"] is None else float(case["dt_bias"].max())) if v.numel() else 0.0
+    d = float(np.log1p(np.exp(most))) if softplus else max(most, 0.0)
+    per_step = 18 + (13 + abs(most)) * d * float(case["A"].abs().max())
+    return T * per_step + N + 40
+
+
+SCANS = [
+    # T, B, C, N, G, type, gate, softplus, dt_bias, D, state, lengths, layout
+    (1, 1, 1, 1, 1, "f32", True, True, True, True, True, None, "time"),
+    (1, 3, 70, 16, 1, "bf16", True, True, True, True, True, None, "slice"),
+    (1, 2, 33, 5, 3, "f16", False, False, False, False, False, None, "batch"),
+    (1, 3, 40, 128, 2, "f32", True, True, True, True, True, [1, 0, 1], "time"),
+    (1, 2, 24, 7, 1, "bf16", True, True, False, True, True, [0, 0], "time"),
+    (2, 2, 64, 4, 1, "f32", True, True, True, True, True, None, "time"),
+    (7, 1, 65, 16, 5, "f32", True, True, True, True, True, None, "time"),
+    (8, 3, 130, 16, 1, "f16", True, True, True, True, True, [8, 3, 0], "slice"),
+    (9, 2, 96, 8, 2, "bf16", False, True, True, False, True, [9, 20], "batch"),
+    (33, 2, 63, 12, 3, "f32", True, False, False, True, False, None, "slice"),
+    (40, 1, 520, 16, 2, "bf16", True, True, True, True, True, None, "time"),
+    (17, 2, 40, 20, 1, "f32", True, True, True, True, True, [17, 8], "time"),
+    (24, 2, 36, 64, 4, "f32", True, True, True, True, True, None, "batch"),
+    (12, 1, 20, 100, 1, "bf16", True, True, True, True, True, None, "time"),
+    (10, 2, 18, 128, 2, "f32", False, True, True, True, True, [10, 9], "slice"),
+    (11, 1, 5, 2, 1, "f32", True, True, True, True, True, [-4], "time"),
+    # divided time: several segments, one of them behind every sample's end
+    (700, 2, 24, 16, 1, "f32", True, True, True, True, True, [333, 257], "time"),
+    (515, 1, 100, 3, 1, "bf16", True, True, True, True, True, None, "slice"),
+    (600, 1, 17, 40, 1, "f32", True, True, True, True, True, [0], "batch"),
+    (300, 3, 10, 8, 2, "f32", False, True, False, False, False, [300, 1, 64], "time"),
+]
+
+
+@pytest.mark.parametrize("T,B,C,N,G,type,gate,softplus,bias,D,state,lengths,layout", SCANS)
+def test_scan_and_its_gradients(T, B, C, N, G, type, gate, softplus, bias, D, state, lengths, layout):
+    ops, dtype = _ops(), TYPES[type]
+    case = _scan_case(T, B, C, N, G, dtype, gate, softplus, bias, D, state, lengths, seed=T * 31 + C)
+    gen = torch.Generator().manual_seed(T + 7)
+    dy, ds = torch.randn((T, B, C), generator=gen).to(dtype), torch.randn((B, C, N), generator=gen)
+    if lengths is not None:
+        for i, n in enumerate(ref.ends_of(lengths, T, B)):
+            dy[n:, i] = float("nan")
+    want = ref.scan(**_double(case), softplus=softplus, lengths=lengths, dy=dy.double(), d_state=ds.double())
+    size = ref.scan(**_double(case), softplus=softplus, lengths=lengths, dy=dy.double(), d_state=ds.double(), absolute=True)
+    seqs = {k: _place(case[k], layout) for k in ("u", "dt", "B", "C", "z")}
+    rest = {k: None if case[k] is None else case[k].cuda() for k in ("D", "dt_bias")}
+    A = case["A"].cuda()
+    ends = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    st = None if case["state"] is None else case["state"].cuda()
+    common = dict(D=rest["D"], z=seqs["z"], dt_bias=rest["dt_bias"], softplus=softplus, lengths=ends)
+    n = _scan_roundings(T, N, C, case, softplus)
+
+    y, s = ops.selective_scan(seqs["u"], seqs["dt"], A, seqs["B"], seqs["C"], state=st, **common)
+    _close(y, want["y"], size["y"], n + 20, "y")
+    _close(s, want["state"], size["state"], n, "state")
+    y2, s2, kept = ops.selective_scan(seqs["u"], seqs["dt"], A, seqs["B"], seqs["C"], state=st, keep=True, **common)
+    _close(y2, want["y"], size["y"], n + 20, "y, states kept")
+    _close(s2, want["state"], size["state"], n, "state, states kept")
+    if T > 1:
+        assert torch.equal(y, y2) and torch.equal(s, s2)
+    # the state in place, the output a range of a wider tensor whose other elements stay as they are
+    if st is not None:
+        own = st.clone()
+        wide = torch.full((T, B, C + 5), 7.0, dtype=dtype, device="cuda")
+        ops.selective_scan(seqs["u"], seqs["dt"], A, seqs["B"], seqs["C"], state=own, state_out=own, out=wide[:, :, 3:3 + C], **common)
+        assert torch.equal(own, s) and torch.equal(wide[:, :, 3:3 + C], y)
+        assert (wide[:, :, :3] == 7.0).all() and (wide[:, :, 3 + C:] == 7.0).all()
+
+    g = ops.selective_scan_backward(_place(dy, layout), seqs["u"], seqs["dt"], A, seqs["B"], seqs["C"], kept, d_state=ds.cuda(), **common)
+    back = 2 * n + 60                                   # forward and backward recurrence, sums over states
+    for name in ("du", "ddt", "dz"):
+        if getattr(g, name) is not None:
+            _close(getattr(g, name), want[name], size[name], back, name)
+    for name in ("dB", "dC"):
+        _close(getattr(g, name), want[name], size[name], back + C, name)
+    for name in ("dA", "dD", "ddt_bias"):
+        if getattr(g, name) is not None:
+            _close(getattr(g, name), want[name], size[name], back + T * B, name)
+        else:
+            assert want[name] is None
+    _close(g.dstate, want["dstate"], size["dstate"], back, "dstate")
+    again = ops.selective_scan_backward(_place(dy, layout), seqs["u"], seqs["dt"], A, seqs["B"], seqs["C"], kept, d_state=ds.cuda(), **common)
+    for a, b in zip(g, again):
+        assert (a is None and b is None) or torch.equal(a, b)
+
+
+def test_scan_without_a_step_and_without_a_sample():
+    ops = _ops()
+    A = -torch.ones((6, 4), device="cuda")
+    for T, B in ((0, 2), (3, 0), (0, 0)):
+        wide, low = torch.zeros((T, B, 6), device="cuda"), torch.zeros((T, B, 1, 4), device="cuda")
+        st = torch.randn((B, 6, 4), device="cuda")
+        y, s, kept = ops.selective_scan(wide, wide, A, low, low, state=st, keep=True)
+        assert y.shape == (T, B, 6) and (T > 0 or torch.equal(s, st))
+        y, s = ops.selective_scan(wide, wide, A, low, low)
+        assert (s == 0).all()
+        g = ops.selective_scan_backward(wide, wide, wide, A, low, low, kept, d_state=st)
+        assert (g.dA == 0).all() and (T > 0 or torch.equal(g.dstate, st))
+
+
+def test_scan_token_by_token_is_the_prompt():
+    """A prompt in one call, in two calls and token by token: the same state within the roundings, and the same outputs."""
+    ops = _ops()
+    T, B, C, N = 70, 3, 90, 16
+    case = _scan_case(T, B, C, N, 1, F32, True, True, True, True, True, None, seed=9)
+    dev = {k: v.cuda() for k, v in case.items()}
+    seqs = lambda a, b: {k: dev[k][a:b] for k in ("u", "dt", "B", "C", "z")}
+    rest = {k: dev[k] for k in ("A", "D", "dt_bias")}
+    want = ref.scan(**_double(case))
+    size = ref.scan(**_double(case), absolute=True)
+    n = _scan_roundings(T, N, C, case, True)
+    for cuts in ([0, T], [0, 33, T], list(range(T + 1))):
+        state, rows = dev["state"].clone(), []
+        for a, b in zip(cuts, cuts[1:]):
+            y, _ = ops.selective_scan(state=state, state_out=state, **seqs(a, b), **rest)
+            rows.append(y)
+        _close(torch.cat(rows), want["y"], size["y"], n + 20, "y in %d calls" % len(rows))
+        _close(state, want["state"], size["state"], n, "state")
+
+
+def test_scan_large_small_and_infinite_values():
+    ops = _ops()
+    # steps so large that nothing of the past is left, and so small that softplus is all that is left of a digit
+    T, B, C, N = 9, 1, 64, 4
+    v = torch.linspace(-80.0, 80.0, T * C).reshape(T, B, C)
+    u, low = torch.ones((T, B, C)), torch.ones((T, B, 1, N))
+    A = -torch.ones((C, N))
+    want = ref.scan(u.double(), v.double(), A.double(), low.double(), low.double())
+    y, s = ops.selective_scan(u.cuda(), v.cuda(), A.cuda(), low.cuda(), low.cuda())
+    assert torch.isfinite(y).all()
+    # every d has 10 + |v| roundings, everything is positive, |v| is at most 80
+    assert ((y.cpu().double() - want["y"]).abs() <= (T * (18 + 93 * 1.0) + 60) * EPS * want["y"]).all()
+    # an infinite input stays in its own channel and sample
+    u = torch.ones((T, 2, C), device="cuda")
+    u[3, 1, 17] = float("inf")
+    dt, low = torch.zeros((T, 2, C), device="cuda"), torch.ones((T, 2, 1, N), device="cuda")
+    y, s = ops.selective_scan(u, dt, A.cuda(), low, low)
+    bad = ~torch.isfinite(y)
+    assert bad[3:, 1, 17].all() and int(bad.sum()) == T - 3 and int((~torch.isfinite(s)).sum()) == N
+
+
+# ---------------------------------------------------------------------------------------------------------------- conv
+
+CONVS = [
+    # T, B, C, K, type, silu, bias, state, lengths, layout
+    (1, 1, 1, 1, "f32", True, True, False, None, "time"),
+    (1, 3, 70, 4, "bf16", True, True, True, None, "slice"),
+    (2, 2, 33, 4, "f32", True, True, True, None, "batch"),
+    (3, 2, 64, 8, "f16", False, False, True, [3, 0], "time"),
+    (5, 2, 520, 4, "bf16", True, True, False, [5, 2], "slice"),
+    (31, 1, 9, 2, "f32", True, True, True, None, "slice"),
+    (32, 2, 16, 3, "f16", True, True, True, [32, 31], "time"),
+    (65, 2, 40, 4, "f32", True, True, True, [64, 33], "batch"),
+    (130, 1, 515, 4, "bf16", True, True, True, None, "slice"),
+    (300, 2, 12, 5, "f32", True, True, True, [300, 129], "time"),
+    (67, 1, 6, 7, "f32", True, True, True, [66], "time"),
+    (260, 1, 8, 6, "bf16", False, True, True, None, "time"),
+    (0, 2, 8, 4, "f32", True, True, True, None, "time"),
+]
+
+
+@pytest.mark.parametrize("T,B,C,K,type,silu,bias,state,lengths,layout", CONVS)
+def test_conv_and_its_gradients(T, B, C, K, type, silu, bias, state, lengths, layout):
+    ops, dtype = _ops(), TYPES[type]
+    gen = torch.Generator().manual_seed(T * 13 + C)
+    normal = lambda *s: torch.randn(s, generator=gen)
+    x, weight, b = normal(T, B, C).to(dtype), normal(C, K), normal(C) if bias else None
+    st = normal(K - 1, B, C).to(dtype) if state else None
+    dy, ds = normal(T, B, C).to(dtype), normal(K - 1, B, C).to(dtype)
+    clean = x.clone()
+    if lengths is not None:
+        for i, n in enumerate(ref.ends_of(lengths, T, B)):
+            x[n:, i] = float("nan")
+            dy[n:, i] = float("inf")
+    args = (x.double(), weight.double(), None if b is None else b.double(), silu, None if st is None else st.double(), lengths)
+    want = ref.conv(*args, dy=dy.double(), d_state=ds.double())
+    size = ref.conv(*args, dy=dy.double(), d_state=ds.double(), absolute=True)
+    put = lambda t: None if t is None else t.cuda()
+    ends = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    xd = _place(x, layout)
+    y, s = ops.causal_conv(xd, put(weight), put(b), silu=silu, state=put(st), lengths=ends)
+    # K + 2 roundings of the sum, whose error the gate multiplies by at most 1.1; the gate's own: |p| <= 60 of them and 8
+    n = 1.1 * (K + 2) + 70
+    _close(y, want["y"], size["y"], n, "y")
+    assert torch.equal(s.cpu().double(), want["state"])
+    if st is not None and K > 1:
+        own = put(st)
+        wide = torch.full((T, B, C + 5), 7.0, dtype=dtype, device="cuda")
+        ops.causal_conv(xd, put(weight), put(b), silu=silu, state=own, state_out=own, lengths=ends, out=wide[:, :, 3:3 + C])
+        assert torch.equal(own, s) and torch.equal(wide[:, :, 3:3 + C], y)
+        assert (wide[:, :, :3] == 7.0).all() and (wide[:, :, 3 + C:] == 7.0).all()
+    back = dict(silu=silu, state=put(st), lengths=ends, d_state=put(ds))
+    g = ops.causal_conv_backward(_place(dy, layout), xd, put(weight), put(b), **back)
+    for got, name, terms in zip(g, ("dx", "dweight", "dbias", "dstate"), (K, T * B, T * B, K)):
+        if got is None:
+            assert want[name] is None
+        else:
+            _close(got, want[name], size[name], n + 10 + terms, name)
+    for a, c in zip(g, ops.causal_conv_backward(_place(dy, layout), xd, put(weight), put(b), **back)):
+        assert (a is None and c is None) or torch.equal(a, c)
+    assert not torch.isnan(clean).any()
+
+
+def test_conv_token_by_token_is_the_prompt():
+    ops = _ops()
+    T, B, C, K = 40, 2, 70, 4
+    gen = torch.Generator().manual_seed(2)
+    x, weight, bias = (torch.randn(s, generator=gen).cuda() for s in ((T, B, C), (C, K), (C,)))
+    x = x.to(BF16)
+    whole, end = ops.causal_conv(x, weight, bias)
+    state = torch.zeros((K - 1, B, C), dtype=BF16, device="cuda")
+    rows = [ops.causal_conv(x[t:t + 1], weight, bias, state=state, state_out=state)[0] for t in range(T)]
+    assert torch.equal(torch.cat(rows), whole) and torch.equal(state, end)
+
+
+# ---------------------------------------------------------------------------------------------------------------- norm
+
+NORMS = [
+    # T, B, W, type, residual type (None: no residual), weight, layout
+    (1, 1, 1, "f32", None, True, "time"),
+    (1, 3, 8, "bf16", "f32", True, "slice"),
+    (3, 2, 127, "f16", "f16", False, "batch"),
+    (2, 2, 128, "bf16", "bf16", True, "time"),
+    (5, 1, 129, "f32", "f32", True, "slice"),
+    (2, 3, 513, "bf16", "f32", True, "batch"),
+    (40, 30, 771, "bf16", "bf16", True, "time"),
+    (2, 1, 4097, "f16", "f32", True, "time"),
+    (2, 2, 8192, "bf16", "bf16", True, "time"),
+    (2, 1, 8200, "f32", "f32", True, "slice"),
+    (1, 2, 16389, "bf16", "f32", True, "time"),
+    (2, 1, 40001, "f16", "f16", True, "time"),
+]
+
+
+def _norm_inputs(T, B, W, type, residual, weight):
+    dtype = TYPES[type]
+    stream = dtype if residual is None else TYPES[residual]
+    gen = torch.Generator().manual_seed(W)
+    normal = lambda *s: torch.randn(s, generator=gen)
+    x = normal(T, B, W).to(dtype)
+    res = None if residual is None else (normal(T, B, W) * 3).to(stream)
+    return dtype, stream, x, res, normal(W) if weight else None, normal(T, B, W).to(dtype), normal(T, B, W).to(stream)
+
+
+# A row's sum: at most 8 + W / 8192 terms one after the other in a lane and pass, 6 and 16 in the joins, one square each;
+# its relative error is halved by the root.  Then the root, a division and two products, four roundings at most each.
+def _norm_roundings(W):
+    return (8 * (1 + W // 8192) + 6 + 16 + 2) / 2 + 10
+
+
+@pytest.mark.parametrize("T,B,W,type,residual,weight,layout", NORMS)
+def test_norm(T, B, W, type, residual, weight, layout):
+    ops = _ops()
+    dtype, stream, x, res, w, _, _ = _norm_inputs(T, B, W, type, residual, weight)
+    put = lambda t: None if t is None else t.cuda()
+    r = x if res is None else (x.float() + res.float()).to(stream)
+    want = ref.norm(r.double(), None if w is None else w.double())
+    n = _norm_roundings(W)
+    wide = None
+    if res is not None:
+        wide = torch.full((T, B, W + 3), 7.0, dtype=stream, device="cuda")
+        wide[:, :, 2:2 + W] = put(res)
+    own = None if wide is None else wide[:, :, 2:2 + W]
+    y, r_out = ops.rms_norm(_place(x, layout), put(w), residual=_place(res, layout))
+    _close(y, want, want, n, "y")
+    assert (r_out is None) if res is None else torch.equal(r_out.cpu(), r)
+    y8, scales, r8 = ops.rms_norm_fp8(_place(x, layout), put(w), residual=own, residual_out=own)      # the stream in place
+    if res is not None:
+        assert r8 is own and torch.equal(own.cpu(), r) and (wide[:, :, :2] == 7.0).all() and (wide[:, :, 2 + W:] == 7.0).all()
+    padded = torch.zeros((T, B, -(-W // 128) * 128), dtype=torch.float64)
+    padded[..., :W] = want
+    amax = padded.view(T, B, -1, 128).abs().amax(-1)
+    _close(scales, amax.clamp(min=2.0 ** -100) / 448.0, amax / 448.0, n + 2, "scales")
+    s = scales.cpu().double().repeat_interleave(128, dim=2)[..., :W]
+    # y over the scale: the norm's roundings and three more, then a rounding to e4m3
+    back = y8.cpu().float().double() * s
+    off = (back - want).abs()
+    bound = want.abs() * (2.0 ** -4 * (1 + (n + 3) * EPS) + (n + 3) * EPS) + s * 2.0 ** -10
+    assert (off <= bound).all(), float((off - bound).max())
+
+
+@pytest.mark.parametrize("T,B,W,type,residual,weight,layout", NORMS + [(700, 3, 24, "f32", "f32", True, "time"), (0, 2, 16, "f32", "f32", True, "time")])
+def test_norm_gradients(T, B, W, type, residual, weight, layout):
+    ops = _ops()
+    dtype, stream, r, _, w, dy, dres = _norm_inputs(T, B, W, type, residual, weight)
+    r = r.to(stream)
+    put = lambda t: None if t is None else t.cuda()
+    add = None if residual is None else dres
+    args = (dy.double(), r.double(), None if w is None else w.double(), 1e-5, None if add is None else add.double())
+    want, size = ref.norm_backward(*args), ref.norm_backward(*args, absolute=True)
+    dr, dw = ops.rms_norm_backward(_place(dy, layout), _place(r, layout), put(w), d_residual=_place(add, layout))
+    n = 3 * _norm_roundings(W) + 10
+    _close(dr, want[0], size[0], n, "dr")
+    if w is None:
+        assert dw is None
+    else:
+        _close(dw, want[1], size[1], n + T * B, "dweight")
+        assert torch.equal(dw, ops.rms_norm_backward(_place(dy, layout), _place(r, layout), put(w), d_residual=_place(add, layout))[1])
+
+
+def test_norm_in_8_bits_of_zeros_tiny_rows_and_nan():
+    ops = _ops()
+    x = torch.zeros((4, 1, 300), device="cuda")
+    x[1] = 1e-30                                         # mean square far below eps
+    x[2, 0, 5] = float("nan")
+    x[3, 0, 7] = float("inf")
+    y, scales, _ = ops.rms_norm_fp8(x)
+    y = y.float()
+    assert (y[0] == 0).all() and torch.equal(scales[0].cpu(), torch.full((1, 3), 2.0 ** -100) / 448.0)
+    back = y[1] * scales[1].repeat_interleave(128, dim=1)[:, :300]
+    assert ((back - x[1] / 1e-5 ** 0.5).abs() <= 2.0 ** -4 * 1.001 * back.abs().max()).all()
+    assert torch.isnan(y[2]).all() and torch.isnan(scales[2]).all()      # the row's mean is none
+    # 1 / sqrt(infinity) is 0: zeros, and 0 times infinity in one place, whose block is NaN
+    assert torch.isnan(y[3, 0, :128]).all() and (y[3, 0, 128:] == 0).all()
+
+
+# ------------------------------------------------------------------------------------------------------ 8-bit projection
+
+PROJECTS = [
+    # T, B, K, R, out type, bias, layout
+    (1, 1, 1, 1, "f32", True, "time"),
+    (1, 1, 128, 16, "bf16", False, "time"),
+    (1, 3, 130, 33, "f16", True, "slice"),
+    (2, 2, 127, 129, "f32", True, "batch"),
+    (1, 8, 1152, 300, "bf16", True, "time"),
+    (5, 7, 400, 257, "f32", True, "slice"),
+    (16, 8, 256, 128, "f32", False, "time"),
+    (43, 3, 384, 384, "bf16", True, "time"),
+    (33, 5, 771, 200, "f32", True, "slice"),
+    (100, 4, 512, 1030, "f16", True, "batch"),
+    (300, 2, 640, 515, "f32", True, "time"),
+    (1, 16, 2304, 5760, "f32", True, "time"),
+    (1, 17, 1000, 2310, "bf16", True, "time"),
+    (1, 64, 1536, 1024, "f32", False, "time"),
+]
+
+
+@pytest.mark.parametrize("T,B,K,R,type,bias,layout", PROJECTS)
+def test_project_fp8(T, B, K, R, type, bias, layout):
+    ops, dtype = _ops(), TYPES[type]
+    gen = torch.Generator().manual_seed(K + R)
+    normal = lambda *s: torch.randn(s, generator=gen, dtype=torch.float64)
+    q, xs = ref.blocks(normal(T * B, K) * (1.0 + 30.0 * torch.rand((T * B, 1), generator=gen, dtype=torch.float64)), 1, 128)
+    w, ws = ref.blocks(normal(R, K) / K ** 0.5, 128, 128)
+    b = normal(R).float() if bias else None
+    want = ref.project(q, xs, w, ws, b).view(T, B, R)
+    size = ref.project(q, xs, w, ws, b, absolute=True).view(T, B, R)
+    x = q.view(T, B, K).view(torch.uint8)
+    x = _place(x, layout, fill=0x7f).view(torch.float8_e4m3fn)          # NaN beside the rows
+    out = ops.project_fp8(x, xs.view(T, B, -1).cuda(), w.cuda(), ws.cuda(), None if b is None else b.cuda(), dtype=dtype)
+    # the sum of a block of 128 exact products, a scale of two, the sum over blocks, the bias
+    n = min(K, 128) + 3 + -(-K // 128) + 2
+    _close(out, want, size, n, "out")
+    wide = torch.full((T, B, R + 5), 7.0, dtype=dtype, device="cuda")
+    ops.project_fp8(x, xs.view(T, B, -1).cuda(), w.cuda(), ws.cuda(), None if b is None else b.cuda(), out=wide[:, :, 3:3 + R])
+    assert torch.equal(wide[:, :, 3:3 + R], out) and (wide[:, :, :3] == 7.0).all() and (wide[:, :, 3 + R:] == 7.0).all()
+
+
+# ---------------------------------------------------------------------------------------------------- offsets and streams
+
+def test_offsets_beyond_32_bits():
+    """Two samples more than 2^32 bytes (and 2^31 elements) apart, and two steps that are far apart."""
+    ops = _ops()
+    T, C, N, K = 3, 64, 16, 4
+    apart = (1 << 31) + 4096
+    base = torch.empty(apart + T * C, dtype=F16, device="cuda")
+    far = lambda: torch.as_strided(base, (T, 2, C), (C, apart, 1))
+    gen = torch.Generator().manual_seed(1)
+    near = torch.randn((T, 2, C), generator=gen).to(F16).cuda()
+    far().copy_(near)
+    weight = torch.randn((C, K), generator=gen).cuda()
+    assert torch.equal(ops.causal_conv(far(), weight)[0], ops.causal_conv(near, weight)[0])
+    assert torch.equal(ops.rms_norm(far())[0], ops.rms_norm(near)[0])
+    A = -torch.rand((C, N), generator=gen).cuda() - 0.1
+    low = torch.randn((T, 2, 1, N), generator=gen).to(F16).cuda()
+    for x in (near, far()):
+        y, s, kept = ops.selective_scan(x, x, A, low, low, z=x, keep=True)
+        g = ops.selective_scan_backward(x, x, x, A, low, low, kept, z=x)
+        if x is near:
+            want = (y, s) + tuple(g)
+        else:
+            for a, b in zip((y, s) + tuple(g), want):
+                assert (a is None and b is None) or torch.equal(a, b)
+    y = ops.selective_scan(far()[:1], far()[:1], A, low[:1], low[:1])[0]
+    assert torch.equal(y, ops.selective_scan(near[:1], near[:1], A, low[:1], low[:1])[0])
+    q, xs = ref.blocks(torch.randn((T * 2, C), generator=gen, dtype=torch.float64), 1, 128)
+    w, ws = ref.blocks(torch.randn((80, C), generator=gen, dtype=torch.float64), 128, 128)
+    bytes_far = torch.as_strided(base.view(torch.uint8), (T, 2, C), (C, apart, 1))
+    bytes_far.copy_(q.view(T, 2, C).view(torch.uint8).cuda())
+    args = (xs.view(T, 2, -1).cuda(), w.cuda(), ws.cuda())
+    assert torch.equal(ops.project_fp8(bytes_far.view(torch.float8_e4m3fn), *args), ops.project_fp8(q.view(T, 2, C).cuda(), *args))
+
+
+def _layer(ops, p, x, res, lengths=None):
+    """Residual, norm and projection in 8 bits, convolution, scan: the front half of a layer as a program runs it."""
+    q, scales, res = ops.rms_norm_fp8(x, p["norm"], residual=res)
+    both = ops.project_fp8(q, scales, p["w"], p["w_scales"], dtype=x.dtype)
+    C = both.shape[2] // 2
+    v, conv_state = ops.causal_conv(both[:, :, :C], p["conv"], p["conv_bias"], lengths=lengths, state=p["conv_state"])
+    y, state = ops.selective_scan(v, p["dt"], p["A"], p["B"], p["C"], D=p["D"], z=both[:, :, C:], dt_bias=p["dt_bias"], lengths=lengths,
+                                  state=p["state"])
+    return y, state, conv_state, res
+
+
+def _layer_inputs(T, B, W, C, N, dtype, seed):
+    gen = torch.Generator().manual_seed(seed)
+    normal = lambda *s: torch.randn(s, generator=gen, dtype=torch.float64)
+    w, ws = ref.blocks(normal(2 * C, W) / W ** 0.5, 128, 128)
+    f = lambda x: x.float().cuda()
+    t = lambda x: x.to(dtype).cuda()
+    p = dict(norm=f(1 + 0.1 * normal(W)), w=w.cuda(), w_scales=ws.cuda(), conv=f(normal(C, 4)), conv_bias=f(normal(C)),
+             conv_state=t(normal(3, B, C)), dt=t(normal(T, B, C)), A=f(-normal(C, N).abs() - 0.1), B=t(normal(T, B, 1, N)),
+             C=t(normal(T, B, 1, N)), D=f(normal(C)), dt_bias=f(normal(C)), state=f(normal(B, C, N)))
+    return p, t(normal(T, B, W)), f(normal(T, B, W))
+
+
+@pytest.mark.parametrize("T", [1, 50])
+def test_a_layer_is_its_operators_one_after_the_other(T):
+    """Each operator's output against its definition on the input that it was given, along the chain."""
+    ops = _ops()
+    B, W, C, N = 3, 200, 96, 16
+    p, x, res = _layer_inputs(T, B, W, C, N, BF16, 5)
+    ends = [T, 0, max(1, T - 7)]
+    lengths = torch.tensor(ends, dtype=torch.int32, device="cuda")
+    y, state, conv_state, r = _layer(ops, p, x, res, lengths)
+    q, scales, r2 = ops.rms_norm_fp8(x, p["norm"], residual=res)
+    assert torch.equal(r, r2) and torch.equal(r, x.float() + res)
+    both = ops.project_fp8(q, scales, p["w"], p["w_scales"], dtype=BF16)
+    cpu = lambda t: t.detach().cpu()
+    args = (cpu(q).view(T * B, W), cpu(scales).view(T * B, -1), cpu(p["w"]), cpu(p["w_scales"]))
+    _close(both, ref.project(*args).view(T, B, -1), ref.project(*args, absolute=True).view(T, B, -1), 128 + 7, "projection")
+    conv_args = (cpu(both[:, :, :C]).double(), cpu(p["conv"]).double(), cpu(p["conv_bias"]).double(), True, cpu(p["conv_state"]).double(), ends)
+    v, _ = ops.causal_conv(both[:, :, :C], p["conv"], p["conv_bias"], lengths=lengths, state=p["conv_state"])
+    _close(v, ref.conv(*conv_args)["y"], ref.conv(*conv_args, absolute=True)["y"], 80, "convolution")
+    case = dict(u=cpu(v), dt=cpu(p["dt"]), A=cpu(p["A"]), B=cpu(p["B"]), C=cpu(p["C"]), D=cpu(p["D"]), z=cpu(both[:, :, C:]),
+                dt_bias=cpu(p["dt_bias"]), state=cpu(p["state"]))
+    n = _scan_roundings(T, N, C, case, True)
+    want, size = ref.scan(**_double(case), lengths=ends), ref.scan(**_double(case), lengths=ends, absolute=True)
+    _close(y, want["y"], size["y"], n + 20, "scan")
+    _close(state, want["state"], size["state"], n, "state")
+
+
+def test_the_8_bit_projection_feeds_a_pruned_layer():
+    """rms_norm_fp8 and project_fp8 in front of SparseRNN.forward: b' in binary32, as project gives it."""
+    from paper_1804_10223_amd import binding, workloads as wl
+    import oracle
+    ops = _ops()
+    w = wl.make_workload("ops-layer", "relu", 256, 4, 12, 0.1, seed=1)
+    gen = torch.Generator().manual_seed(8)
+    x = torch.randn((12, 4, 192), generator=gen).cuda()
+    wq, ws = ref.blocks(torch.randn((256, 192), generator=gen, dtype=torch.float64) / 14.0, 128, 128)
+    q, scales, _ = ops.rms_norm_fp8(x)
+    b = ops.project_fp8(q, scales, wq.cuda(), ws.cuda())
+    with binding.SparseRNN(w.hidden, w.batch, w.cell, w.row_ptr, w.col_idx, w.val_bits) as rnn:
+        h = rnn.forward(b)
+        assert rnn.check() == 0
+    want = oracle.rnn_forward(w.hidden, w.batch, w.cell, w.row_ptr, w.col_idx, w.val_bits, b.cpu().numpy(), None)
+    for t in range(12):
+        assert np.abs(h[t].cpu().numpy() - want[t]).max() <= 1e-3 * np.abs(want[t]).max()
+
+
+def _training_step(ops, p, x, res, dy, ds):
+    r = x.float() + res
+    n, r = ops.rms_norm(x, p["norm"], residual=res)
+    v, cs = ops.causal_conv(n, p["conv"], p["conv_bias"])
+    y, state, kept = ops.selective_scan(v, p["dt"], p["A"], p["B"], p["C"], D=p["D"], z=n, dt_bias=p["dt_bias"], keep=True)
+    g = ops.selective_scan_backward(dy, v, p["dt"], p["A"], p["B"], p["C"], kept, D=p["D"], z=n, dt_bias=p["dt_bias"], d_state=ds)
+    dx, dw, db, _ = ops.causal_conv_backward(g.du, n, p["conv"], p["conv_bias"])
+    dr, dnorm = ops.rms_norm_backward(dx + g.dz, r, p["norm"])
+    return (y, state, dr, dnorm, dw, db) + tuple(g)
+
+
+def test_a_training_step_through_all_of_them():
+    """norm -> convolution -> scan (gated by the norm's output) and back, against autograd through the definitions."""
+    ops = _ops()
+    T, B, C, N = 21, 2, 48, 8
+    p, x, res = _layer_inputs(T, B, C, C, N, F32, 6)
+    gen = torch.Generator().manual_seed(3)
+    dy, ds = torch.randn((T, B, C), generator=gen), torch.randn((B, C, N), generator=gen)
+    got = _training_step(ops, p, x, res, dy.cuda(), ds.cuda())
+    leaf = lambda t: t.detach().cpu().double().requires_grad_()
+    r, norm, w, b, dt, A, Bm, Cm, D, bias = [leaf(t) for t in (x + res, p["norm"], p["conv"], p["conv_bias"], p["dt"], p["A"], p["B"], p["C"], p["D"], p["dt_bias"])]
+    n = ref.norm(r, norm)
+    out = ref.scan(ref.conv(n, w, b)["y"], dt, A, Bm, Cm, D, n, bias)
+    want = torch.autograd.grad((out["y"] * dy.double()).sum() + (out["state"] * ds.double()).sum(), (r, norm, w, b, dt, A, Bm, Cm, D, bias))
+    have = (got[2], got[3], got[4], got[5], got[7], got[8], got[9], got[10], got[11], got[13])
+    for a, e in zip(have, want):
+        # four operators' worth of roundings, some hundred each, of results of the size of the largest one
+        assert ((a.cpu().double() - e).abs() <= 4 * 400 * EPS * e.abs().max() * 8).all()
+
+
+def _same(a, b):
+    return all((x is None and y is None) or torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_captured_calls_replay_like_eager_ones():
+    """One graph with everything in it, replayed between eager calls, on new inputs each time; a second graph beside it."""
+    ops = _ops()
+    T, B, C, N = 300, 1, 96, 16                       # divided time: workspaces inside the graph
+    p, x, res = _layer_inputs(T, B, C, C // 2 * 2, N, F32, 7)
+    q, x2, res2 = _layer_inputs(T, B, C, C, N, F32, 17)
+    gen = torch.Generator().manual_seed(4)
+    dy, ds = torch.randn((T, B, C), generator=gen).cuda(), torch.randn((B, C, N), generator=gen).cuda()
+
+    def everything(p, x):
+        return tuple(_layer(ops, {**p, "w": p["w"], "conv_state": None, "state": None}, x, res)) + _training_step(ops, p, x, res, dy, ds)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graphs = []
+    with torch.cuda.stream(side):
+        for params, inputs in ((p, x), (q, x2)):
+            everything(params, inputs)
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                outputs = everything(params, inputs)
+            graphs.append((graph, outputs, params, inputs))
+    torch.cuda.current_stream().wait_stream(side)
+    for turn in range(4):
+        for graph, outputs, params, inputs in graphs:
+            inputs.copy_(torch.randn(inputs.shape, generator=gen))
+            want = everything(params, inputs)
+            for o in outputs:
+                if o is not None and o.dtype != torch.float8_e4m3fn:
+                    o.fill_(float("nan"))
+            graph.replay()
+            torch.cuda.synchronize()
+            assert _same(outputs, want), turn
+    for graph, outputs, params, inputs in graphs:     # both in flight, on two streams
+        outputs[0].fill_(float("nan"))
+    want = [everything(params, inputs) for _, _, params, inputs in graphs]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        graphs[1][0].replay()
+    graphs[0][0].replay()
+    torch.cuda.synchronize()
+    assert _same(graphs[0][1], want[0]) and _same(graphs[1][1], want[1])
+
+
+def test_calls_on_two_streams_at_once():
+    ops = _ops()
+    T, B, C, N = 600, 1, 128, 16
+    inputs = [_layer_inputs(T, B, C, C, N, F32, s) for s in (11, 12)]
+    dy, ds = torch.randn((T, B, C), device="cuda"), torch.randn((B, C, N), device="cuda")
+    want = [_training_step(ops, p, x, res, dy, ds) for p, x, res in inputs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in inputs]
+    got = []
+    for _ in range(3):
+        for stream, (p, x, res) in zip(streams, inputs):
+            with torch.cuda.stream(stream):
+                got.append(_training_step(ops, p, x, res, dy, ds))
+    torch.cuda.synchronize()
+    for i, g in enumerate(got):
+        assert _same(g, want[i % 2]), i
+
+
+def test_python_refusals():
+    ops = _ops()
+    x = torch.zeros((2, 1, 8), device="cuda")
+    low, A = torch.zeros((2, 1, 1, 4), device="cuda"), torch.zeros((8, 4), device="cuda")
+    w = torch.zeros((8, 4), device="cuda")
+    q = torch.zeros((2, 1, 8), dtype=torch.float8_e4m3fn, device="cuda")
+    one = torch.ones((2, 1, 1), device="cuda")
+    for error, call in (
+            (ValueError, lambda: ops.selective_scan(x[0], x, A, low, low)),
+            (ValueError, lambda: ops.selective_scan(x, x[:1], A, low, low)),
+            (TypeError, lambda: ops.selective_scan(x, x.half(), A, low, low)),
+            (TypeError, lambda: ops.selective_scan(x.double(), x, A, low, low)),
+            (TypeError, lambda: ops.selective_scan(x, x, None, low, low)),
+            (ValueError, lambda: ops.selective_scan(x, x, A.t().contiguous(), low, low)),
+            (TypeError, lambda: ops.selective_scan(x, x, A, low, low.cpu())),
+            (TypeError, lambda: ops.selective_scan(x.transpose(0, 2), x.transpose(0, 2), A[:2], low, low)),
+            (TypeError, lambda: ops.selective_scan(x, x, A, low, low, lengths=torch.ones(1, device="cuda"))),
+            (TypeError, lambda: ops.selective_scan_backward(x, x, x, A, low, low, None)),
+            (ValueError, lambda: ops.selective_scan_backward(x, x, x, A, low, low, torch.zeros(3, dtype=torch.uint8, device="cuda"))),
+            (ValueError, lambda: ops.causal_conv(x, w[:4])),
+            (ops.SprnnError, lambda: ops.causal_conv(x, torch.zeros((8, 9), device="cuda"))),
+            (TypeError, lambda: ops.causal_conv(x.half(), w, state=torch.zeros((3, 1, 8), device="cuda"))),
+            (TypeError, lambda: ops.rms_norm(x.half(), residual=x.bfloat16())),
+            (ValueError, lambda: ops.rms_norm(x[0])),
+            (ops.SprnnError, lambda: ops.rms_norm(x, eps=-1.0)),
+            (TypeError, lambda: ops.rms_norm_backward(x, None)),
+            (TypeError, lambda: ops.project_fp8(x, one, q[0], one[0])),
+            (TypeError, lambda: ops.project_fp8(q, one, q[:, 0], one[0], dtype=torch.float64)),
+            (ValueError, lambda: ops.project_fp8(q, one, q[:, 0], one)),
+            (TypeError, lambda: ops.project_fp8(q, one, q[:, 0], one[0], dtype=F16, out=x))):
+        with pytest.raises(error):
+            call()
