@@ -27,6 +27,7 @@ struct ScanShape {
   int T, B, C, N, G;
   int per_group;                       // channels that share B and C
   int quads;
+  int states, lanes;                   // of the forward pass: states that a lane holds, lanes that share a channel
   int segments, segment;               // segments of time and their steps (a multiple of kTile)
   int back_segments, back_segment;     // ... of the backward pass
   int64_t state_floats() const { return (int64_t)B * quads * C * 4; }
@@ -77,11 +78,13 @@ struct Cursor {
   uint32_t step;                       // bytes between rows
   __device__ __forceinline__ Cursor(const View<E>& v, int t, int b, int offset = 0)
       : base(reinterpret_cast<uint64_t>(v.data + ((int64_t)t * v.step + (int64_t)b * v.sample + offset))), step((uint32_t)v.step * (uint32_t)sizeof(E)) {}
-  // (width: elements of a row, 0 where there is no tensor)
+  // (width: elements of a row, 0 where there is no tensor.  FRESH: the compiler is to form offsets where they are used; kept
+  // for eight rows of seven tensors they fill the registers that the states of the backward pass are in.)
+  template <bool FRESH = false>
   __device__ __forceinline__ Tile<E> tile(int rows, int width) const {
     rows = min(rows, kTile);
-    uint32_t own_step = step;            // offsets are formed where they are used: kept for every row of every tensor they
-    asm volatile("" : "+s"(own_step));   // would fill the registers that the states are in
+    uint32_t own_step = step;
+    if (FRESH) asm volatile("" : "+s"(own_step));
     const uint32_t bytes = width > 0 && rows > 0 ? (uint32_t)(rows - 1) * own_step + (uint32_t)width * (uint32_t)sizeof(E) : 0u;
     const uint64_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)base), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(base >> 32));
     return Tile<E>{__builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(lo | hi << 32), 0, __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000), own_step};
@@ -108,16 +111,38 @@ struct States {
   }
 };
 
-// d from v = dt + dt_bias.  exp(v) with the rounding of v log2(e) taken back, log1p by the rounding of 1 + e taken back:
-// both would otherwise cost the small steps (v far below 0) their last digits.
+// d from v = dt + dt_bias: max(v, 0) + log1p(exp(-|v|)).  exp's argument v log2(e) and the sum 1 + e are rounded, which would
+// cost small steps (v far below 0) their last digits; what the roundings took is added to the results again (to log1p
+// undivided by 1 + e: off by less than e 2^-24).
 __device__ __forceinline__ float softplus(float v) {
-  const float hi = v * kLog2e;
-  const float lo = __builtin_fmaf(v, kLog2e, -hi) + v * 1.925963033500e-08f;
+  const float m = -__builtin_fabsf(v);
+  const float hi = m * kLog2e, lo = __builtin_fmaf(m, kLog2e, -hi);
   float e = exp2_fast(hi);
   e = __builtin_fmaf(e, lo * kLn2, e);
-  const float s = 1.0f + e, back = s - 1.0f;
-  const float log1p = __builtin_amdgcn_logf(s) * kLn2 * (e * __builtin_amdgcn_rcpf(back));
-  return v > 20.0f ? v : back == 0.0f ? e : log1p;
+  const float s = 1.0f + e;
+  return fmaxf(v, 0.0f) + __builtin_fmaf(__builtin_amdgcn_logf(s), kLn2, e - (s - 1.0f));
+}
+
+// a = exp(d A), with A times log2(e) at hand.  v_exp_f32 is 0.11 x 2^-24 low on average for results just below 1 (measured
+// over arguments from -1e-2 on; 0.31 x 2^-24 in the root mean square), and a slow state multiplies by a thousand such results
+// in a row: 7e-6 of its value.  The argument is raised by as much, which costs nothing in a multiply-add, leaves exp(0) at 1
+// and is below half a step of arguments that matter less.
+constexpr float kRaise = 1.0e-8f;
+__device__ __forceinline__ float decay(float d, float A) { return exp2_fast(__builtin_fmaf(d, A, kRaise)); }
+
+// Step q's value out of S neighbouring lanes, of which lane q % S holds it.
+template <int S>
+__device__ __forceinline__ float from_owner(float v, int q) {
+  const int bits = __builtin_bit_cast(int, v);
+  if constexpr (S == 1) return v;
+  else if constexpr (S == 2)
+    return __builtin_bit_cast(float, q % 2 ? __builtin_amdgcn_mov_dpp(bits, 0xf5, 0xf, 0xf, true) : __builtin_amdgcn_mov_dpp(bits, 0xa0, 0xf, 0xf, true));
+  else if constexpr (S == 4)
+    return __builtin_bit_cast(float, q % 4 == 0   ? __builtin_amdgcn_mov_dpp(bits, 0x00, 0xf, 0xf, true)
+                                     : q % 4 == 1 ? __builtin_amdgcn_mov_dpp(bits, 0x55, 0xf, 0xf, true)
+                                     : q % 4 == 2 ? __builtin_amdgcn_mov_dpp(bits, 0xaa, 0xf, 0xf, true)
+                                                  : __builtin_amdgcn_mov_dpp(bits, 0xff, 0xf, 0xf, true));
+  else return __shfl(v, ((threadIdx.x & 63) & ~(S - 1)) | (q % S));
 }
 
 // The end states of segments 1.. (run from zero) chained into the true states in front of every segment:

@@ -1,26 +1,36 @@
 // Forward pass of the selective scan (see sprnn_scan.h for the mathematics) and its C entry points.
 #include "sprnn_scan.h"
 
+// Splits of a channel's states over lanes: states a lane, lanes.
+#define EVERY_SPLIT CASE(8, 1) CASE(16, 1) CASE(4, 2) CASE(8, 2) CASE(16, 2) CASE(4, 4) CASE(8, 4) CASE(16, 4) CASE(16, 8)
+
 namespace sprnn {
 namespace {
 
-// Prompts.  A wavefront owns 64 / S channels of one sample (and group) and a segment of time; a lane holds NS states of a
-// channel, S lanes share one.  B and C of a tile of steps are the same for all its channels: they are brought into LDS in
-// binary32 once a tile, and u, dt and z of the next tile are in flight while a tile is worked through.
+int blocks_of(const ScanShape& s) { return (s.per_group + 63) / 64; }
+
+// Prompts.  A workgroup owns 64 channels of one sample (and group) and a segment of time; S lanes share a channel, a lane
+// holds NS of its states, so there are S wavefronts.  Everything that depends on (step, channel) alone is computed once:
+// the S lanes of a channel share out the steps of a tile, and hand d and d u over to their neighbours.  B and C of a tile
+// are the same for all channels and are brought into LDS in binary32 once a tile; the next tile's loads are in flight while
+// a tile is worked through, and two LDS buffers make one barrier a tile enough.
 // LOCAL: a segment's effect only (H[segment + 1] from a zero state, sums[segment] = sum of d).
 template <int TYPE, int NS, int S, bool LOCAL>
-__global__ __launch_bounds__(64) void scan_kernel(ScanArgs a, View<const Element<TYPE>> us, View<const Element<TYPE>> dts,
-                                                  View<const Element<TYPE>> zs, View<const Element<TYPE>> Bs,
-                                                  View<const Element<TYPE>> Cs, const float* state_in, View<Element<TYPE>> ys,
-                                                  float* state_out, float* kept, float* H, float* sums) {
+__global__ __launch_bounds__(64 * S) void scan_kernel(ScanArgs a, View<const Element<TYPE>> us, View<const Element<TYPE>> dts,
+                                                      View<const Element<TYPE>> zs, View<const Element<TYPE>> Bs,
+                                                      View<const Element<TYPE>> Cs, const float* state_in, View<Element<TYPE>> ys,
+                                                      float* state_out, float* kept, float* H, float* sums) {
   typedef Element<TYPE> E;
-  constexpr int kN = NS * S, kOwn = kTile * kN / 64;   // of B; as many of C
-  static_assert(kTile * kN % 64 == 0, "the tile's states are dealt out evenly");
+  constexpr int kN = NS * S, kItems = kTile / S;
+  constexpr int kOwn = kTile * kN / (64 * S) > 0 ? kTile * kN / (64 * S) : 1;   // elements of B (and of C) that a lane brings
+  constexpr int kAhead = 2;          // tiles whose inputs are in flight (even: the LDS buffers take turns)
+  constexpr bool kHalf = kTile * kN < 64 * S;    // four states a lane: two lanes bring the same one (no branch around a load in flight)
+  static_assert(S <= kTile && (kHalf || kTile * kN % (64 * S) == 0), "steps and states are dealt out evenly");
   __shared__ __attribute__((aligned(16))) float low[2][LOCAL ? 1 : 2][kTile][kN];
-  const int lane = threadIdx.x, sub = lane % S;
+  const int tid = threadIdx.x, sub = tid % S;
   const int group = blockIdx.x / a.blocks, block = blockIdx.x - group * a.blocks;
   const int b = blockIdx.y, seg = blockIdx.z;
-  const int in_group = block * (64 / S) + lane / S;
+  const int in_group = block * 64 + tid / S;
   const bool mine = in_group < a.per_group;
   const int c = group * a.per_group + min(in_group, a.per_group - 1);
   const int t0 = seg * a.segment, t1 = min(t0 + a.segment, a.T), end = sample_end(a.lengths, b, a.T);
@@ -57,86 +67,111 @@ __global__ __launch_bounds__(64) void scan_kernel(ScanArgs a, View<const Element
   };
   const float D = !LOCAL && a.D ? a.D[c] : 0.0f, bias = a.dt_bias ? a.dt_bias[c] : 0.0f;
 
-  E u[kTile], dt[kTile], z[kTile];
-  E own_B[kOwn], own_C[kOwn];
+  // this lane's steps of a tile are sub, sub + S, ..
+  struct Inputs {
+    E u[kItems], dt[kItems], z[kItems], own_B[kOwn], own_C[kOwn];
+  };
   Cursor<const E> u_at(us, t0, b), dt_at(dts, t0, b), z_at(zs, t0, b);
   Cursor<const E> B_at(Bs, t0, b, group * a.N), C_at(Cs, t0, b, group * a.N);
   Cursor<E> y_at(ys, t0, b);
   const bool gated = zs.data != nullptr;
-  auto fetch = [&](int rows) {
+  auto fetch = [&](Inputs& in, int rows) {
     const Tile<const E> u_rows = u_at.tile(rows, a.C), dt_rows = dt_at.tile(rows, a.C), z_rows = z_at.tile(rows, gated ? a.C : 0);
     const Tile<const E> B_rows = B_at.tile(rows, a.N), C_rows = C_at.tile(rows, a.N);
     u_at.forth(); dt_at.forth(); z_at.forth(); B_at.forth(); C_at.forth();
 #pragma unroll
-    for (int q = 0; q < kTile; ++q) {
-      u[q] = u_rows.load(q, c);
-      dt[q] = dt_rows.load(q, c);
-      if (!LOCAL) z[q] = z_rows.load(q, c);
+    for (int i = 0; i < kItems; ++i) {
+      in.u[i] = u_rows.load(i * S + sub, c);
+      in.dt[i] = dt_rows.load(i * S + sub, c);
+      if (!LOCAL) in.z[i] = z_rows.load(i * S + sub, c);
     }
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
-      const int at = i * 64 + lane;
-      own_B[i] = B_rows.load(at / kN, at % kN);
-      if (!LOCAL) own_C[i] = C_rows.load(at / kN, at % kN);
+      const int at = (i * 64 * S + tid) % (kTile * kN);
+      in.own_B[i] = B_rows.load(at / kN, at % kN);
+      if (!LOCAL) in.own_C[i] = C_rows.load(at / kN, at % kN);
     }
   };
   float total = 0.0f;
-  fetch(live - t0);
-  int buffer = 0;
-  for (int t = t0; t < live; t += kTile, buffer ^= 1) {
+  auto work = [&](Inputs& in, int t, int buffer) {           // one tile; its inputs are followed by those of kAhead tiles on
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
-      const int at = i * 64 + lane;
-      const bool in = at % kN < a.N && t + at / kN < live;   // neither the next group's states nor what lies behind the end
-      (&low[buffer][0][0][0])[at] = in ? (float)own_B[i] : 0.0f;
-      if (!LOCAL) (&low[buffer][LOCAL ? 0 : 1][0][0])[at] = in ? (float)own_C[i] : 0.0f;
+      const int at = (i * 64 * S + tid) % (kTile * kN);
+      const bool there = at % kN < a.N && t + at / kN < live;   // neither the next group's states nor what lies behind the end
+      (&low[buffer][0][0][0])[at] = there ? (float)in.own_B[i] : 0.0f;
+      if (!LOCAL) (&low[buffer][LOCAL ? 0 : 1][0][0])[at] = there ? (float)in.own_C[i] : 0.0f;
     }
-    if (kept && mine) put_states(kept, t / kTile);
-    float d[kTile], x[kTile], gate[kTile], skip[kTile];
+    if (kept && mine && t < live) put_states(kept, t / kTile);
+    float d[kItems], x[kItems], gate[kItems], skip[kItems], y[kItems];
 #pragma unroll
-    for (int q = 0; q < kTile; ++q) {
-      const float v = (float)dt[q] + bias;
-      const bool in = t + q < live;
-      const float uq = in ? (float)u[q] : 0.0f;
-      d[q] = in ? a.softplus ? softplus(v) : v : 0.0f;
-      x[q] = d[q] * uq;
-      skip[q] = D * uq;
-      const float g = (float)z[q];
-      gate[q] = gated ? g * sigmoid(g) : 1.0f;
+    for (int i = 0; i < kItems; ++i) d[i] = (float)in.dt[i] + bias;
+    if (a.softplus) {
+#pragma unroll
+      for (int i = 0; i < kItems; ++i) d[i] = softplus(d[i]);
     }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    fetch(live - t - kTile);
-    const Tile<E> y_rows = y_at.tile(live - t, a.C);
-    y_at.forth();
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const bool there = t + i * S + sub < live;
+      const float ui = there ? (float)in.u[i] : 0.0f;
+      d[i] = there ? d[i] : 0.0f;
+      x[i] = d[i] * ui;
+      skip[i] = D * ui;
+      if (LOCAL) total += d[i];
+    }
+    if (!LOCAL) {
+#pragma unroll
+      for (int i = 0; i < kItems; ++i) gate[i] = 1.0f;
+      if (gated) {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) gate[i] = (float)in.z[i] * sigmoid((float)in.z[i]);
+      }
+    }
+    __syncthreads();
+    fetch(in, live - t - kAhead * kTile);
 #pragma unroll
     for (int q = 0; q < kTile; ++q) {
       const float* const Bq = &low[buffer][0][q][sub * NS];
       const float* const Cq = &low[buffer][LOCAL ? 0 : 1][q][sub * NS];
-      float y = 0.0f;
+      const float dq = from_owner<S>(d[q / S], q), xq = from_owner<S>(x[q / S], q);
+      float sum = 0.0f;
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
-        h[i] = exp2_fast(d[q] * A[i]) * h[i] + x[q] * Bq[i];
-        if (!LOCAL) y += Cq[i] * h[i];
+        h[i] = decay(dq, A[i]) * h[i] + xq * Bq[i];
+        if (!LOCAL) sum += Cq[i] * h[i];
       }
-      if (LOCAL) {
-        total += d[q];
-      } else {
-        y = (sum_lanes<S>(y) + skip[q]) * gate[q];
-        if (S == 1 && mine) y_rows.store(q, c, y);
-        else if (sub == q % S && mine) y_rows.store(q, c, y);
+      if (!LOCAL) {
+        sum = sum_lanes<S>(sum);
+        y[q / S] = S == 1 || sub == q % S ? sum : q % S ? y[q / S] : 0.0f;
+        if (S == 1) asm volatile("" : "+v"(y[q / S]));   // formed here, not where it is stored with all its factors alive till then
       }
     }
+    if (!LOCAL) {
+      const Tile<E> y_rows = y_at.tile(live - t, a.C);
+      y_at.forth();
+      if (mine) {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) y_rows.store(i * S + sub, c, (y[i] + skip[i]) * gate[i]);
+      }
+    }
+  };
+  // A tile takes a wavefront about as long as a load from memory when few wavefronts share a SIMD.
+  Inputs ring[kAhead];
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) fetch(ring[k], live - t0 - k * kTile);
+  // (whole rounds of kAhead tiles, without a branch that a load in flight would have to be waited for: tiles behind the end
+  // multiply the states by one and store nothing)
+  for (int t = t0; t < live; t += kAhead * kTile) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) work(ring[k], t + k * kTile, k & 1);
   }
   if (!mine) return;
   if (LOCAL) {
     put_states(H, seg + 1);
+    total = sum_lanes<S>(total);
     if (sub == 0) sums[((int64_t)seg * a.B + b) * a.C + c] = total;
     return;
   }
-  if (sub == 0)
-    for (int t = max(t0, end); t < t1; ++t) ys.row(t, b)[c] = (E)0.0f;
+  for (int t = max(t0, end) + sub; t < t1; t += S) ys.row(t, b)[c] = (E)0.0f;
   // the segment that holds the sample's last step has its last state
   if (state_out && (end > t0 || t0 == 0) && end <= t1) {
 #pragma unroll
@@ -148,8 +183,8 @@ __global__ __launch_bounds__(64) void scan_kernel(ScanArgs a, View<const Element
 }
 
 // One lane per (sample, channel, quad of states).
-__global__ __launch_bounds__(256) void chain_kernel(ScanArgs a, int segments, const float* first, float* H, const float* sums) {
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__global__ __launch_bounds__(64) void chain_kernel(ScanArgs a, int segments, const float* first, float* H, const float* sums) {
+  const int64_t at = (int64_t)blockIdx.x * 64 + threadIdx.x;
   const int64_t lanes = (int64_t)a.B * a.quads * a.C;
   if (at >= lanes) return;
   const int c = (int)(at % a.C), quad = (int)(at / a.C % a.quads), b = (int)(at / ((int64_t)a.C * a.quads));
@@ -160,18 +195,28 @@ __global__ __launch_bounds__(256) void chain_kernel(ScanArgs a, int segments, co
     A[i] = n < a.N ? a.A[(int64_t)c * a.N + n] * kLog2e : 0.0f;
     h[i] = first && n < a.N ? first[((int64_t)b * a.C + c) * a.N + n] : 0.0f;
   }
-  for (int s = 0; s < segments; ++s) {
-    float* const slot = H + ((int64_t)s * lanes + at) * 4;
-    Pack<float, 4> p;
-    if (s > 0) {
-      p = load_pack<4>(slot);
-      const float total = sums[((int64_t)(s - 1) * a.B + b) * a.C + c];
+  auto slot = [&](int s) { return H + ((int64_t)s * lanes + at) * 4; };
+  Pack<float, 4> front;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) h[i] = exp2_fast(A[i] * total) * h[i] + p.v[i];
+  for (int i = 0; i < 4; ++i) front.v[i] = h[i];
+  store_pack(slot(0), front);
+  constexpr int kAhead = 8;                                // loads do not depend on the chain: eight segments in flight
+  for (int s = 1; s < segments; s += kAhead) {
+    Pack<float, 4> p[kAhead];
+    float total[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int from = min(s + k, segments - 1);
+      p[k] = load_pack<4>(slot(from));
+      total[k] = sums[((int64_t)(from - 1) * a.B + b) * a.C + c];
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) p.v[i] = h[i];
-    store_pack(slot, p);
+    for (int k = 0; k < kAhead; ++k) {
+      if (s + k >= segments) break;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[k].v[i] = h[i] = exp2_fast(A[i] * total[k]) * h[i] + p[k].v[i];
+      store_pack(slot(s + k), p[k]);
+    }
   }
 }
 
@@ -213,7 +258,7 @@ __global__ __launch_bounds__(64) void scan_token_kernel(ScanArgs a, View<const E
     const float d = a.softplus ? softplus(v) : v, x = d * u;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      h.v[i] = exp2_fast(d * (A.v[i] * kLog2e)) * h.v[i] + x * (float)Bn.v[i];
+      h.v[i] = decay(d, A.v[i] * kLog2e) * h.v[i] + x * (float)Bn.v[i];
       y += (float)Cn.v[i] * h.v[i];
     }
     y = sum_lanes<S>(y) + D * u;
@@ -230,9 +275,9 @@ template <int TYPE, int NS, int S>
 hipError_t run_prompt(ScanArgs a, const ScanShape& s, const sprnn_scan_t* p, const float* state_in, const sprnn_seq_t& y, float* state_out,
                       float* kept, float* H, float* sums, hipStream_t stream) {
   typedef Element<TYPE> E;
-  a.blocks = (s.per_group + 64 / S - 1) / (64 / S);
+  a.blocks = blocks_of(s);
   const View<const E> u = view<const E>(p->u), dt = view<const E>(p->dt), z = view<const E>(p->z), B = view<const E>(p->B), C = view<const E>(p->C);
-  const dim3 block(64);
+  const dim3 block(64 * S);
   if (s.segments > 1) {
     hipError_t e = launch(scan_kernel<TYPE, NS, S, true>, dim3((unsigned)(a.blocks * s.G), (unsigned)s.B, (unsigned)s.segments - 1), block, 0, stream,
                           a, u, dt, z, B, C, (const float*)nullptr, view<E>(y), (float*)nullptr, (float*)nullptr, H, sums);
@@ -264,11 +309,11 @@ hipError_t run_scan(const ScanShape& s, const sprnn_scan_t* p, const float* stat
   }
   float* const H = workspace;
   float* const sums = workspace + s.segments * s.state_floats();
-  return s.N <= 8 ? run_prompt<TYPE, 8, 1>(a, s, p, state_in, y, state_out, kept, H, sums, stream)
-       : s.N <= 16 ? run_prompt<TYPE, 16, 1>(a, s, p, state_in, y, state_out, kept, H, sums, stream)
-       : s.N <= 32 ? run_prompt<TYPE, 16, 2>(a, s, p, state_in, y, state_out, kept, H, sums, stream)
-       : s.N <= 64 ? run_prompt<TYPE, 16, 4>(a, s, p, state_in, y, state_out, kept, H, sums, stream)
-                   : run_prompt<TYPE, 16, 8>(a, s, p, state_in, y, state_out, kept, H, sums, stream);
+#define CASE(NS, S) \
+  if (s.states == NS && s.lanes == S) return run_prompt<TYPE, NS, S>(a, s, p, state_in, y, state_out, kept, H, sums, stream);
+  EVERY_SPLIT
+#undef CASE
+  return hipErrorInvalidValue;
 }
 
 int round_up(int n, int to) { return (n + to - 1) / to * to; }
@@ -277,27 +322,33 @@ int round_up(int n, int to) { return (n + to - 1) / to * to; }
 
 hipError_t launch_chain(const ScanArgs& a, int segments, const float* first, float* H, const float* sums, hipStream_t stream) {
   const int64_t lanes = (int64_t)a.B * a.quads * a.C;
-  return launch(chain_kernel, dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, stream, a, segments, first, H, sums);
+  return launch(chain_kernel, dim3((unsigned)((lanes + 63) / 64)), dim3(64), 0, stream, a, segments, first, H, sums);
 }
 
-// A wavefront per 64 states' lanes and sample runs at its best rate with one or two wavefronts a SIMD; below half a
-// wavefront a SIMD two runs over divided time (1.9 times the work) win.
+// How many lanes share a channel: as few as its states need (16 a lane at most), and more, down to four states a lane, while
+// there are fewer wavefronts than twice the SIMDs: sharing costs a tenth more instructions (8 x 2048 x 4608, 16 states: 850 us
+// with one lane a channel, 576 wavefronts).  Where that is not enough time is divided, which costs nearly twice the work.
 ScanShape scan_shape(const sprnn_scan_t* p) {
   ScanShape s{};
   s.T = p->steps; s.B = p->batch; s.C = p->channels; s.N = p->states; s.G = p->groups;
   s.per_group = s.C / s.G;
   s.quads = (s.N + 3) / 4;
+  const int64_t columns = (int64_t)s.G * blocks_of(s) * s.B;      // workgroups of a segment
+  s.lanes = 1;
+  while (16 * s.lanes < s.N) s.lanes *= 2;
+  while (s.lanes < 4 && 4 * s.lanes < s.N && columns * s.lanes < 2 * kSimds) s.lanes *= 2;
+  s.states = 4;
+  while (s.states * s.lanes < s.N) s.states *= 2;
+  if (s.states * s.lanes < 8) s.states = 8;
   auto divide = [&](int64_t waves, int* segments, int* segment) {
-    int64_t n = waves > 0 ? 2 * kSimds / waves : 1;
+    int64_t n = waves > 0 ? 4 * kSimds / waves : 1;
     n = n < s.T / 64 ? n : s.T / 64;
     if (n < 4) n = 1;
     *segment = round_up(s.T > 0 ? (int)((s.T + n - 1) / n) : 1, kTile);
     *segments = s.T > 0 ? (s.T + *segment - 1) / *segment : 1;
   };
-  const int lanes = s.N <= 16 ? 1 : s.N <= 32 ? 2 : s.N <= 64 ? 4 : 8;
-  const int64_t waves = (int64_t)s.G * ((s.per_group + 64 / lanes - 1) / (64 / lanes)) * s.B;
-  divide(waves, &s.segments, &s.segment);
-  divide(waves, &s.back_segments, &s.back_segment);
+  divide(columns * s.lanes, &s.segments, &s.segment);
+  divide(columns, &s.back_segments, &s.back_segment);
   return s;
 }
 

@@ -86,7 +86,7 @@ __global__ __launch_bounds__(64) void scan_adjoint_kernel(ScanArgs a, int segmen
 #pragma unroll
     for (int q = kTile - 1; q >= 0; --q) {
 #pragma unroll
-      for (int i = 0; i < NS; ++i) g[i] = exp2_fast(d[q] * A[i]) * (g[i] + low[buffer][q][sub * NS + i] * e[q]);
+      for (int i = 0; i < NS; ++i) g[i] = decay(d[q], A[i]) * (g[i] + low[buffer][q][sub * NS + i] * e[q]);
       total += d[q];
     }
   }
@@ -214,13 +214,13 @@ __global__ __launch_bounds__(64 * waves_of(S), 2) void scan_backward_kernel(Scan
   for (int t = last; t >= t0 && live > t0; t -= kTile, buffer ^= 1) {
     // what depends on (step, channel) alone
     {
-      const Tile<const E> u_rows = u_at.tile(live - t, a.C), dt_rows = dt_at.tile(live - t, a.C), z_rows = z_at.tile(live - t, gated ? a.C : 0), dy_rows = dy_at.tile(live - t, a.C);
+      const Tile<const E> u_rows = u_at.template tile<true>(live - t, a.C), dt_rows = dt_at.template tile<true>(live - t, a.C), z_rows = z_at.template tile<true>(live - t, gated ? a.C : 0), dy_rows = dy_at.template tile<true>(live - t, a.C);
       E u[kItems], dt[kItems], z[kItems], dy[kItems];
       load_items<CW>(u, u_rows, lane, c_item);
       load_items<CW>(dt, dt_rows, lane, c_item);
       load_items<CW>(z, z_rows, lane, c_item);
       load_items<CW>(dy, dy_rows, lane, c_item);
-      const Tile<const E> B_rows = B_at.tile(live - t, a.N), C_rows = C_at.tile(live - t, a.N);
+      const Tile<const E> B_rows = B_at.template tile<true>(live - t, a.N), C_rows = C_at.template tile<true>(live - t, a.N);
       B_at.back(); C_at.back();
       for (int i = threadIdx.x; i < kTile * kRow; i += 64 * W) {
         const int n = i % kRow, q = i / kRow;
@@ -264,7 +264,7 @@ __global__ __launch_bounds__(64 * waves_of(S), 2) void scan_backward_kernel(Scan
         const floatx4_t Bq = *reinterpret_cast<const floatx4_t*>(&low[buffer][q][0][at]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          f[q][i] = exp2_fast(d * A[r][i]);
+          f[q][i] = decay(d, A[r][i]);
           h[q][i] = f[q][i] * (q ? h[q ? q - 1 : 0][i] : start[i]) + x * Bq[i];
         }
       }
@@ -319,10 +319,10 @@ __global__ __launch_bounds__(64 * waves_of(S), 2) void scan_backward_kernel(Scan
       if (t + q < live) partial[((((int64_t)block * a.T + t + q) * a.B + b) * a.G + group) * (2 * kRow) + i % (2 * kRow)] = sum;
     }
     // gradients of what depends on (step, channel) alone
-    const Tile<E> du_rows = du_at.tile(live - t, io.du.data ? a.C : 0), ddt_rows = ddt_at.tile(live - t, io.ddt.data ? a.C : 0), dz_rows = dz_at.tile(live - t, io.dz.data ? a.C : 0);
+    const Tile<E> du_rows = du_at.template tile<true>(live - t, io.du.data ? a.C : 0), ddt_rows = ddt_at.template tile<true>(live - t, io.ddt.data ? a.C : 0), dz_rows = dz_at.template tile<true>(live - t, io.dz.data ? a.C : 0);
     du_at.back(); ddt_at.back(); dz_at.back();
     if (owned(item_channel)) {
-      const Tile<const E> u_rows = u_at.tile(live - t, a.C), dt_rows = dt_at.tile(live - t, a.C), z_rows = z_at.tile(live - t, gated ? a.C : 0), dy_rows = dy_at.tile(live - t, a.C);
+      const Tile<const E> u_rows = u_at.template tile<true>(live - t, a.C), dt_rows = dt_at.template tile<true>(live - t, a.C), z_rows = z_at.template tile<true>(live - t, gated ? a.C : 0), dy_rows = dy_at.template tile<true>(live - t, a.C);
       E us[kItems], dts[kItems], zs[kItems], dys[kItems];
       load_items<CW>(us, u_rows, lane, c_item);
       load_items<CW>(dts, dt_rows, lane, c_item);
