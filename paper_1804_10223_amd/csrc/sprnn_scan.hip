@@ -14,13 +14,16 @@ int blocks_of(const ScanShape& s) { return (s.per_group + 63) / 64; }
 // the S lanes of a channel share out the steps of a tile, and hand d and d u over to their neighbours.  B and C of a tile
 // are the same for all channels and are brought into LDS in binary32 once a tile; the next tile's loads are in flight while
 // a tile is worked through, and two LDS buffers make one barrier a tile enough.
-// LOCAL: a segment's effect only (H[segment + 1] from a zero state, sums[segment] = sum of d).
-template <int TYPE, int NS, int S, bool LOCAL>
+// kLocal: a segment's effect only (H[segment + 1] from a zero state, sums[segment] = sum of d).
+enum { kPlain, kKeeping, kLocal };     // what a run of the forward pass leaves: y; y and the states in front of every tile; its effect
+
+template <int TYPE, int NS, int S, int MODE>
 __global__ __launch_bounds__(64 * S) void scan_kernel(ScanArgs a, View<const Element<TYPE>> us, View<const Element<TYPE>> dts,
                                                       View<const Element<TYPE>> zs, View<const Element<TYPE>> Bs,
                                                       View<const Element<TYPE>> Cs, const float* state_in, View<Element<TYPE>> ys,
                                                       float* state_out, float* kept, float* H, float* sums) {
   typedef Element<TYPE> E;
+  constexpr bool LOCAL = MODE == kLocal;
   constexpr int kN = NS * S, kItems = kTile / S;
   constexpr int kOwn = kTile * kN / (64 * S) > 0 ? kTile * kN / (64 * S) : 1;   // elements of B (and of C) that a lane brings
   constexpr int kAhead = 2;          // tiles whose inputs are in flight (even: the LDS buffers take turns)
@@ -101,7 +104,7 @@ __global__ __launch_bounds__(64 * S) void scan_kernel(ScanArgs a, View<const Ele
       (&low[buffer][0][0][0])[at] = there ? (float)in.own_B[i] : 0.0f;
       if (!LOCAL) (&low[buffer][LOCAL ? 0 : 1][0][0])[at] = there ? (float)in.own_C[i] : 0.0f;
     }
-    if (kept && mine && t < live) put_states(kept, t / kTile);
+    if (MODE == kKeeping && mine && t < live) put_states(kept, t / kTile);
     float d[kItems], x[kItems], gate[kItems], skip[kItems], y[kItems];
 #pragma unroll
     for (int i = 0; i < kItems; ++i) d[i] = (float)in.dt[i] + bias;
@@ -279,7 +282,7 @@ hipError_t run_prompt(ScanArgs a, const ScanShape& s, const sprnn_scan_t* p, con
   const View<const E> u = view<const E>(p->u), dt = view<const E>(p->dt), z = view<const E>(p->z), B = view<const E>(p->B), C = view<const E>(p->C);
   const dim3 block(64 * S);
   if (s.segments > 1) {
-    hipError_t e = launch(scan_kernel<TYPE, NS, S, true>, dim3((unsigned)(a.blocks * s.G), (unsigned)s.B, (unsigned)s.segments - 1), block, 0, stream,
+    hipError_t e = launch(scan_kernel<TYPE, NS, S, kLocal>, dim3((unsigned)(a.blocks * s.G), (unsigned)s.B, (unsigned)s.segments - 1), block, 0, stream,
                           a, u, dt, z, B, C, (const float*)nullptr, view<E>(y), (float*)nullptr, (float*)nullptr, H, sums);
     if (e != hipSuccess) return e;
     e = launch_chain(a, s.segments, state_in, H, sums, stream);
@@ -287,7 +290,7 @@ hipError_t run_prompt(ScanArgs a, const ScanShape& s, const sprnn_scan_t* p, con
   } else {
     H = nullptr;
   }
-  return launch(scan_kernel<TYPE, NS, S, false>, dim3((unsigned)(a.blocks * s.G), (unsigned)s.B, (unsigned)s.segments), block, 0, stream, a, u,
+  return launch(kept ? scan_kernel<TYPE, NS, S, kKeeping> : scan_kernel<TYPE, NS, S, kPlain>, dim3((unsigned)(a.blocks * s.G), (unsigned)s.B, (unsigned)s.segments), block, 0, stream, a, u,
                 dt, z, B, C, state_in, view<E>(y), state_out, kept, H, sums);
 }
 

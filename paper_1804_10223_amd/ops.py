@@ -11,44 +11,31 @@ passes are calls of their own, like those of ``SparseRNN``.
 from __future__ import annotations
 
 import ctypes
+import functools
+import struct
 from typing import NamedTuple, Optional
+
+import torch
 
 from .binding import SPRNN_OK, SprnnError, load_library
 
-TYPES = {"float32": 0, "float16": 1, "bfloat16": 2, "float8_e4m3fn": 3}
+TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.float8_e4m3fn: 3}
+F32, E4M3 = torch.float32, torch.float8_e4m3fn
 
 
 class Seq(ctypes.Structure):
+    """sprnn_seq_t, passed by value."""
     _fields_ = [("data", ctypes.c_void_p), ("step", ctypes.c_int64), ("sample", ctypes.c_int64)]
 
 
-class Scan(ctypes.Structure):
-    _fields_ = [("steps", ctypes.c_int), ("batch", ctypes.c_int), ("channels", ctypes.c_int), ("states", ctypes.c_int),
-                ("groups", ctypes.c_int), ("type", ctypes.c_int), ("softplus", ctypes.c_int),
-                ("u", Seq), ("dt", Seq), ("z", Seq), ("B", Seq), ("C", Seq),
-                ("A", ctypes.c_void_p), ("D", ctypes.c_void_p), ("dt_bias", ctypes.c_void_p), ("lengths", ctypes.c_void_p)]
-
-
-class ScanGradientBuffers(ctypes.Structure):
-    _fields_ = [("u", Seq), ("dt", Seq), ("z", Seq), ("B", Seq), ("C", Seq),
-                ("A", ctypes.c_void_p), ("D", ctypes.c_void_p), ("dt_bias", ctypes.c_void_p), ("state", ctypes.c_void_p)]
-
-
-class Conv(ctypes.Structure):
-    _fields_ = [("steps", ctypes.c_int), ("batch", ctypes.c_int), ("channels", ctypes.c_int), ("width", ctypes.c_int),
-                ("type", ctypes.c_int), ("silu", ctypes.c_int), ("x", Seq),
-                ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("state", ctypes.c_void_p), ("lengths", ctypes.c_void_p)]
-
-
-class Norm(ctypes.Structure):
-    _fields_ = [("steps", ctypes.c_int), ("batch", ctypes.c_int), ("width", ctypes.c_int), ("type", ctypes.c_int),
-                ("residual_type", ctypes.c_int), ("eps", ctypes.c_float), ("weight", ctypes.c_void_p)]
-
-
-class Product(ctypes.Structure):
-    _fields_ = [("steps", ctypes.c_int), ("batch", ctypes.c_int), ("rows", ctypes.c_int), ("inputs", ctypes.c_int),
-                ("x", Seq), ("x_scales", ctypes.c_void_p), ("w", ctypes.c_void_p), ("w_scales", ctypes.c_void_p),
-                ("bias", ctypes.c_void_p)]
+# The structures of the C ABI as bytes (a ctypes structure takes five times as long to fill, more than a token's kernels run).
+# Addresses are 0 where there is nothing; a view is its address and the strides of its first two dimensions.
+_SCAN = struct.Struct("7i4x" + 5 * "Qqq" + "4Q")               # sprnn_scan_t
+_SCAN_GRADIENTS = struct.Struct(5 * "Qqq" + "4Q")              # sprnn_scan_gradients_t
+_CONV = struct.Struct("6iQqq4Q")                               # sprnn_conv_t
+_NORM = struct.Struct("5ifQ")                                  # sprnn_norm_t
+_PRODUCT = struct.Struct("4iQqq4Q")                            # sprnn_product_t
+_NOTHING = (0, 0, 0)
 
 
 class ScanGradients(NamedTuple):
@@ -72,17 +59,16 @@ def _library():
     if _lib is None:
         lib = load_library()
         vp, ci, i64, i64p = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.POINTER(ctypes.c_int64)
-        P = ctypes.POINTER
-        for name, args in (("sprnn_scan_sizes", [P(Scan), i64p, i64p, i64p]),
-                           ("sprnn_scan_forward", [ci, P(Scan), vp, Seq, vp, vp, vp, i64, vp]),
-                           ("sprnn_scan_backward", [ci, P(Scan), Seq, vp, vp, P(ScanGradientBuffers), vp, i64, vp]),
-                           ("sprnn_conv_forward", [ci, P(Conv), Seq, vp, vp]),
-                           ("sprnn_conv_sizes", [P(Conv), i64p]),
-                           ("sprnn_conv_backward", [ci, P(Conv), Seq, vp, Seq, vp, vp, vp, vp, i64, vp]),
-                           ("sprnn_rms_norm", [ci, P(Norm), Seq, Seq, Seq, ci, Seq, vp, vp]),
-                           ("sprnn_rms_norm_sizes", [P(Norm), i64p]),
-                           ("sprnn_rms_norm_backward", [ci, P(Norm), Seq, Seq, Seq, Seq, vp, vp, i64, vp]),
-                           ("sprnn_project_quantized", [ci, P(Product), ci, Seq, vp])):
+        for name, args in (("sprnn_scan_sizes", [vp, i64p, i64p, i64p]),
+                           ("sprnn_scan_forward", [ci, vp, vp, Seq, vp, vp, vp, i64, vp]),
+                           ("sprnn_scan_backward", [ci, vp, Seq, vp, vp, vp, vp, i64, vp]),
+                           ("sprnn_conv_forward", [ci, vp, Seq, vp, vp]),
+                           ("sprnn_conv_sizes", [vp, i64p]),
+                           ("sprnn_conv_backward", [ci, vp, Seq, vp, Seq, vp, vp, vp, vp, i64, vp]),
+                           ("sprnn_rms_norm", [ci, vp, Seq, Seq, Seq, ci, Seq, vp, vp]),
+                           ("sprnn_rms_norm_sizes", [vp, i64p]),
+                           ("sprnn_rms_norm_backward", [ci, vp, Seq, Seq, Seq, Seq, vp, vp, i64, vp]),
+                           ("sprnn_project_quantized", [ci, vp, ci, Seq, vp])):
             function = getattr(lib, name)
             function.restype, function.argtypes = ci, args
         _lib = lib
@@ -94,91 +80,102 @@ def _check(rc, what):
         raise SprnnError(rc, what)
 
 
-def _type(dtype, what, also=()):
-    name = str(dtype).replace("torch.", "")
-    if name not in ("float32", "float16", "bfloat16") and name not in also:
-        raise TypeError("%s must be float32, float16 or bfloat16%s, got %s" % (what, "".join(", " + a for a in also), name))
-    return TYPES[name]
+def _name(dtype):
+    return str(dtype).replace("torch.", "")
 
 
-class _Call:
-    """The device, stream and shape checks that the arguments of one call share."""
+def _type(dtype, what):
+    code = TYPES.get(dtype, 3)
+    if code == 3:
+        raise TypeError("%s must be float32, float16 or bfloat16, got %s" % (what, _name(dtype)))
+    return code
 
-    def __init__(self, first, what):
-        import torch
-        self.torch = torch
-        if not (isinstance(first, torch.Tensor) and first.is_cuda):
-            raise TypeError("%s must be a CUDA tensor" % what)
-        self.device = first.device
-        self.index = first.device.index
 
-    def stream(self):
-        return ctypes.c_void_p(self.torch.cuda.current_stream(self.device).cuda_stream)
+def _index(t, what):
+    """The GPU that a call's first tensor is on."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        raise TypeError("%s must be a CUDA tensor" % what)
+    return t.get_device()
 
-    def empty(self, shape, dtype):
-        return self.torch.empty(shape, dtype=dtype, device=self.device)
 
-    def workspace(self, size):
-        """A buffer of this call alone: torch's allocator hands it on in stream order, and a captured graph has its own."""
-        return self.empty((max(int(size), 1),), self.torch.uint8)
+def _stream(index):
+    """hipStream_t of torch's current stream (without the Stream object that torch.cuda.current_stream makes, 2 us)."""
+    return torch._C._cuda_getCurrentRawStream(index)
 
-    def _tensor(self, t, shape, dtype, what):
-        if not (isinstance(t, self.torch.Tensor) and t.device == self.device and t.dtype == dtype):
-            raise TypeError("%s must be a %s tensor on %s" % (what, str(dtype).replace("torch.", ""), self.device))
-        if tuple(t.shape) != tuple(shape):
-            raise ValueError("%s must have shape %s, got %s" % (what, tuple(shape), tuple(t.shape)))
 
-    def plain(self, t, shape, dtype, what):
-        """Address of a contiguous tensor, or None."""
-        if t is None:
-            return None
-        self._tensor(t, shape, dtype, what)
-        if not t.is_contiguous():
-            raise TypeError("%s must be contiguous" % what)
-        return ctypes.c_void_p(t.data_ptr())
+def _refuse(t, shape, dtype, index, what):
+    if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.get_device() == index):
+        raise TypeError("%s must be a %s tensor on cuda:%d" % (what, _name(dtype), index))
+    raise ValueError("%s must have shape %s, got %s" % (what, tuple(shape), tuple(t.shape)))
 
-    def seq(self, t, shape, dtype, what):
-        """View of a tensor [T, B, ...] whose dimensions behind the second are contiguous, or of none."""
-        if t is None:
-            return Seq(None, 0, 0)
-        self._tensor(t, shape, dtype, what)
-        inner = 1
-        for d in range(len(shape) - 1, 1, -1):
-            if shape[d] > 1 and t.stride(d) != inner:
-                raise TypeError("%s must be contiguous behind its first two dimensions" % what)
-            inner *= shape[d]
-        return Seq(t.data_ptr(), t.stride(0), t.stride(1))
 
-    def lengths(self, t, batch):
-        return self.plain(t, (batch,), self.torch.int32, "lengths")
+def _plain(t, shape, dtype, index, what):
+    """Address of a contiguous tensor, 0 for None."""
+    if t is None:
+        return 0
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == index):
+        _refuse(t, shape, dtype, index, what)
+    if not t.is_contiguous():
+        raise TypeError("%s must be contiguous" % what)
+    return t.data_ptr()
+
+
+def _seq(t, shape, dtype, index, what):
+    """(address, strides of the first two dimensions) of a tensor [T, B, ...] that is contiguous behind them."""
+    if t is None:
+        return _NOTHING
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == index):
+        _refuse(t, shape, dtype, index, what)
+    strides = t.stride()
+    if len(strides) == 3:
+        if strides[2] != 1 and shape[2] != 1:
+            raise TypeError("%s must be contiguous behind its first two dimensions" % what)
+    elif (strides[3] != 1 and shape[3] != 1) or (strides[2] != shape[3] and shape[2] != 1):
+        raise TypeError("%s must be contiguous behind its first two dimensions" % what)
+    return t.data_ptr(), strides[0], strides[1]
+
+
+def _workspace(size, device):
+    """A buffer of one call alone: torch's allocator hands it on in stream order, and a captured graph has its own."""
+    return torch.empty((size,), dtype=torch.uint8, device=device) if size else None
+
+
+def _at(t):
+    return 0 if t is None else t.data_ptr()
+
+
+@functools.lru_cache(maxsize=256)
+def _sizes(function, head, count):
+    """Bytes of the buffers of a call of these sizes (they follow from the sizes alone)."""
+    sizes = [ctypes.c_int64() for _ in range(count)]
+    _check(getattr(_library(), function)(head, *[ctypes.byref(x) for x in sizes]), function)
+    return tuple(x.value for x in sizes)
 
 
 # ------------------------------------------------------------------------------------------------------- selective scan
 
-def _scan(call, u, dt, A, B, C, D, z, dt_bias, softplus, lengths):
-    f32 = call.torch.float32
-    if u.dim() != 3 or B.dim() != 4:
-        raise ValueError("u must be [T, B, C] and B must be [T, B, groups, N]")
-    T, batch, channels = u.shape
-    groups, states = B.shape[2], B.shape[3]
-    s = Scan(T, batch, channels, states, groups, _type(u.dtype, "u"), 1 if softplus else 0)
-    wide, low = (T, batch, channels), (T, batch, groups, states)
-    s.u, s.dt, s.z = call.seq(u, wide, u.dtype, "u"), call.seq(dt, wide, u.dtype, "dt"), call.seq(z, wide, u.dtype, "z")
-    s.B, s.C = call.seq(B, low, u.dtype, "B"), call.seq(C, low, u.dtype, "C")
-    if A is None:
-        raise TypeError("A must be a float32 tensor on %s" % call.device)
-    s.A = call.plain(A, (channels, states), f32, "A")
-    s.D, s.dt_bias = call.plain(D, (channels,), f32, "D"), call.plain(dt_bias, (channels,), f32, "dt_bias")
-    s.lengths = call.lengths(lengths, batch)
-    return s
-
-
 def scan_sizes(steps, batch, channels, states, groups=1):
     """sprnn_scan_sizes: bytes of (forward workspace, backward workspace, what the forward pass keeps)."""
-    s = Scan(steps, batch, channels, states, groups)
-    sizes = [ctypes.c_int64() for _ in range(3)]
-    _check(_library().sprnn_scan_sizes(ctypes.byref(s), *[ctypes.byref(x) for x in sizes]), "sprnn_scan_sizes")
-    return tuple(x.value for x in sizes)
+    return _sizes("sprnn_scan_sizes", _SCAN.pack(steps, batch, channels, states, groups, *([0] * 21)), 3)
+
+
+def _scan(index, u, dt, A, B, C, D, z, dt_bias, softplus, lengths):
+    """sprnn_scan_t and the sizes (T, batch, C, N, groups)."""
+    if u.dim() != 3 or B is None or B.dim() != 4:
+        raise ValueError("u must be [T, B, C] and B must be [T, B, groups, N]")
+    dtype = u.dtype
+    wide, low = u.shape, B.shape
+    T, batch, channels = wide
+    groups, states = low[2], low[3]
+    low = (T, batch, groups, states)
+    if A is None or dt is None or C is None:
+        raise TypeError("dt, A and C must be tensors on cuda:%d" % index)
+    packed = _SCAN.pack(T, batch, channels, states, groups, _type(dtype, "u"), 1 if softplus else 0,
+                        *_seq(u, wide, dtype, index, "u"), *_seq(dt, wide, dtype, index, "dt"), *_seq(z, wide, dtype, index, "z"),
+                        *_seq(B, low, dtype, index, "B"), *_seq(C, low, dtype, index, "C"),
+                        _plain(A, (channels, states), F32, index, "A"), _plain(D, (channels,), F32, index, "D"),
+                        _plain(dt_bias, (channels,), F32, index, "dt_bias"), _plain(lengths, (batch,), torch.int32, index, "lengths"))
+    return packed, T, batch, channels, states, groups
 
 
 def selective_scan(u, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=True, state=None, lengths=None, keep=False,
@@ -186,20 +183,19 @@ def selective_scan(u, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=True, 
     """sprnn_scan_forward: u, dt, z [T, B, C], A [C, N], B, C [T, B, groups, N], D, dt_bias [C], state [B, C, N]
     -> (y [T, B, C], state behind the last step [B, C, N]), with keep=True also what selective_scan_backward reads.
     state_out may be state itself (the next token of running sequences: T = 1 with the state in place)."""
-    call = _Call(u, "u")
-    s = _scan(call, u, dt, A, B, C, D, z, dt_bias, softplus, lengths)
-    f32, full = call.torch.float32, (s.batch, s.channels, s.states)
+    index = _index(u, "u")
+    scan, T, batch, channels, states, groups = _scan(index, u, dt, A, B, C, D, z, dt_bias, softplus, lengths)
+    dtype, device, full = u.dtype, u.device, (batch, channels, states)
     if out is None:
-        out = call.empty((s.steps, s.batch, s.channels), u.dtype)
+        out = torch.empty((T, batch, channels), dtype=dtype, device=device)
     if state_out is None:
-        state_out = call.empty(full, f32)
-    need, _, kept_bytes = scan_sizes(s.steps, s.batch, s.channels, s.states, s.groups)
-    workspace = call.workspace(need)
-    kept = call.workspace(kept_bytes) if keep else None
-    rc = _library().sprnn_scan_forward(call.index, ctypes.byref(s), call.plain(state, full, f32, "state"),
-                                       call.seq(out, (s.steps, s.batch, s.channels), u.dtype, "out"),
-                                       call.plain(state_out, full, f32, "state_out"), kept.data_ptr() if keep else None,
-                                       workspace.data_ptr(), workspace.numel(), call.stream())
+        state_out = torch.empty(full, dtype=F32, device=device)
+    need, _, kept_bytes = scan_sizes(T, batch, channels, states, groups)
+    workspace = _workspace(need, device)
+    kept = torch.empty((kept_bytes,), dtype=torch.uint8, device=device) if keep else None
+    rc = _library().sprnn_scan_forward(index, scan, _plain(state, full, F32, index, "state"),
+                                       Seq(*_seq(out, (T, batch, channels), dtype, index, "out")),
+                                       _plain(state_out, full, F32, index, "state_out"), _at(kept), _at(workspace), need, _stream(index))
     _check(rc, "sprnn_scan_forward")
     return (out, state_out, kept) if keep else (out, state_out)
 
@@ -207,57 +203,55 @@ def selective_scan(u, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=True, 
 def selective_scan_backward(dy, u, dt, A, B, C, kept, D=None, z=None, dt_bias=None, softplus=True, lengths=None, d_state=None):
     """sprnn_scan_backward: gradients of selective_scan(..., keep=True) for dy [T, B, C] and d_state [B, C, N] (gradient of
     the state behind the last step) -> ScanGradients."""
-    call = _Call(u, "u")
-    s = _scan(call, u, dt, A, B, C, D, z, dt_bias, softplus, lengths)
-    f32, wide, low, full = call.torch.float32, (s.steps, s.batch, s.channels), (s.steps, s.batch, s.groups, s.states), (s.batch, s.channels, s.states)
-    _, need, kept_bytes = scan_sizes(s.steps, s.batch, s.channels, s.states, s.groups)
-    kept_at = call.plain(kept, (max(kept_bytes, 1),), call.torch.uint8, "kept")
-    if kept_at is None:
+    index = _index(u, "u")
+    scan, T, batch, channels, states, groups = _scan(index, u, dt, A, B, C, D, z, dt_bias, softplus, lengths)
+    dtype, device = u.dtype, u.device
+    wide, low, full = (T, batch, channels), (T, batch, groups, states), (batch, channels, states)
+    _, need, kept_bytes = scan_sizes(T, batch, channels, states, groups)
+    if kept is None:
         raise TypeError("kept must be what selective_scan(..., keep=True) returned")
-    g = ScanGradients(call.empty(wide, u.dtype), call.empty(wide, u.dtype), call.empty((s.channels, s.states), f32),
-                      call.empty(low, u.dtype), call.empty(low, u.dtype), None if D is None else call.empty((s.channels,), f32),
-                      None if z is None else call.empty(wide, u.dtype), None if dt_bias is None else call.empty((s.channels,), f32),
-                      call.empty(full, f32))
-    at = lambda t: None if t is None else t.data_ptr()
-    b = ScanGradientBuffers(call.seq(g.du, wide, u.dtype, "du"), call.seq(g.ddt, wide, u.dtype, "ddt"), call.seq(g.dz, wide, u.dtype, "dz"),
-                            call.seq(g.dB, low, u.dtype, "dB"), call.seq(g.dC, low, u.dtype, "dC"),
-                            at(g.dA), at(g.dD), at(g.ddt_bias), at(g.dstate))
-    workspace = call.workspace(need)
-    rc = _library().sprnn_scan_backward(call.index, ctypes.byref(s), call.seq(dy, wide, u.dtype, "dy"),
-                                        call.plain(d_state, full, f32, "d_state"), kept_at, ctypes.byref(b),
-                                        workspace.data_ptr(), workspace.numel(), call.stream())
+    kept_at = _plain(kept, (kept_bytes,), torch.uint8, index, "kept")
+    empty = lambda shape, type: torch.empty(shape, dtype=type, device=device)
+    g = ScanGradients(empty(wide, dtype), empty(wide, dtype), empty((channels, states), F32), empty(low, dtype), empty(low, dtype),
+                      None if D is None else empty((channels,), F32), None if z is None else empty(wide, dtype),
+                      None if dt_bias is None else empty((channels,), F32), empty(full, F32))
+    rows = lambda t: _NOTHING if t is None else (t.data_ptr(),) + t.stride()[:2]
+    buffers = _SCAN_GRADIENTS.pack(*rows(g.du), *rows(g.ddt), *rows(g.dz), *rows(g.dB), *rows(g.dC), _at(g.dA), _at(g.dD), _at(g.ddt_bias),
+                                   _at(g.dstate))
+    workspace = _workspace(need, device)
+    rc = _library().sprnn_scan_backward(index, scan, Seq(*_seq(dy, wide, dtype, index, "dy")), _plain(d_state, full, F32, index, "d_state"),
+                                        kept_at, buffers, _at(workspace), need, _stream(index))
     _check(rc, "sprnn_scan_backward")
     return g
 
 
 # ---------------------------------------------------------------------------------------------------- causal convolution
 
-def _conv(call, x, weight, bias, silu, state, lengths):
-    f32 = call.torch.float32
-    if x.dim() != 3 or weight.dim() != 2:
+def _conv(index, x, weight, bias, silu, state, lengths):
+    """sprnn_conv_t and the sizes (T, batch, C, K)."""
+    if x.dim() != 3 or weight is None or weight.dim() != 2:
         raise ValueError("x must be [T, B, C] and weight must be [C, K]")
     T, batch, channels = x.shape
     width = weight.shape[1]
-    c = Conv(T, batch, channels, width, _type(x.dtype, "x"), 1 if silu else 0)
-    c.x = call.seq(x, (T, batch, channels), x.dtype, "x")
-    c.weight, c.bias = call.plain(weight, (channels, width), f32, "weight"), call.plain(bias, (channels,), f32, "bias")
-    c.state = call.plain(state, (max(width - 1, 0), batch, channels), x.dtype, "state")
-    c.lengths = call.lengths(lengths, batch)
-    return c
+    packed = _CONV.pack(T, batch, channels, width, _type(x.dtype, "x"), 1 if silu else 0, *_seq(x, x.shape, x.dtype, index, "x"),
+                        _plain(weight, (channels, width), F32, index, "weight"), _plain(bias, (channels,), F32, index, "bias"),
+                        _plain(state, (max(width - 1, 0), batch, channels), x.dtype, index, "state"),
+                        _plain(lengths, (batch,), torch.int32, index, "lengths"))
+    return packed, T, batch, channels, width
 
 
 def causal_conv(x, weight, bias=None, silu=True, state=None, lengths=None, out=None, state_out=None):
     """sprnn_conv_forward: x [T, B, C], weight [C, K] (K 1..8), bias [C], state [K - 1, B, C] (the inputs before step 0)
     -> (y [T, B, C], the last K - 1 inputs [K - 1, B, C]).  state_out may be state itself."""
-    call = _Call(x, "x")
-    c = _conv(call, x, weight, bias, silu, state, lengths)
-    wide, past = (c.steps, c.batch, c.channels), (max(c.width - 1, 0), c.batch, c.channels)
+    index = _index(x, "x")
+    conv, T, batch, channels, width = _conv(index, x, weight, bias, silu, state, lengths)
+    dtype, wide, past = x.dtype, (T, batch, channels), (max(width - 1, 0), batch, channels)
     if out is None:
-        out = call.empty(wide, x.dtype)
+        out = torch.empty(wide, dtype=dtype, device=x.device)
     if state_out is None:
-        state_out = call.empty(past, x.dtype)
-    rc = _library().sprnn_conv_forward(call.index, ctypes.byref(c), call.seq(out, wide, x.dtype, "out"),
-                                       call.plain(state_out, past, x.dtype, "state_out"), call.stream())
+        state_out = torch.empty(past, dtype=dtype, device=x.device)
+    rc = _library().sprnn_conv_forward(index, conv, Seq(*_seq(out, wide, dtype, index, "out")),
+                                       _plain(state_out, past, dtype, index, "state_out"), _stream(index))
     _check(rc, "sprnn_conv_forward")
     return out, state_out
 
@@ -265,50 +259,47 @@ def causal_conv(x, weight, bias=None, silu=True, state=None, lengths=None, out=N
 def causal_conv_backward(dy, x, weight, bias=None, silu=True, state=None, lengths=None, d_state=None):
     """sprnn_conv_backward: (dx [T, B, C], dweight [C, K], dbias [C] or None, dstate [K - 1, B, C]) of causal_conv for dy
     [T, B, C] and d_state [K - 1, B, C], the gradient of the state it returned."""
-    call = _Call(x, "x")
-    c = _conv(call, x, weight, bias, silu, state, lengths)
-    f32, wide, past = call.torch.float32, (c.steps, c.batch, c.channels), (max(c.width - 1, 0), c.batch, c.channels)
-    need = ctypes.c_int64()
-    _check(_library().sprnn_conv_sizes(ctypes.byref(c), ctypes.byref(need)), "sprnn_conv_sizes")
-    workspace = call.workspace(need.value)
-    dx, dweight, dstate = call.empty(wide, x.dtype), call.empty((c.channels, c.width), f32), call.empty(past, x.dtype)
-    dbias = None if bias is None else call.empty((c.channels,), f32)
-    rc = _library().sprnn_conv_backward(call.index, ctypes.byref(c), call.seq(dy, wide, x.dtype, "dy"),
-                                        call.plain(d_state, past, x.dtype, "d_state"), call.seq(dx, wide, x.dtype, "dx"),
-                                        dweight.data_ptr(), None if dbias is None else dbias.data_ptr(), dstate.data_ptr(),
-                                        workspace.data_ptr(), workspace.numel(), call.stream())
+    index = _index(x, "x")
+    conv, T, batch, channels, width = _conv(index, x, weight, bias, silu, state, lengths)
+    dtype, device, wide, past = x.dtype, x.device, (T, batch, channels), (max(width - 1, 0), batch, channels)
+    (need,) = _sizes("sprnn_conv_sizes", _CONV.pack(T, batch, channels, width, *([0] * 9)), 1)
+    workspace = _workspace(need, device)
+    dx, dstate = torch.empty(wide, dtype=dtype, device=device), torch.empty(past, dtype=dtype, device=device)
+    dweight = torch.empty((channels, width), dtype=F32, device=device)
+    dbias = None if bias is None else torch.empty((channels,), dtype=F32, device=device)
+    rc = _library().sprnn_conv_backward(index, conv, Seq(*_seq(dy, wide, dtype, index, "dy")), _plain(d_state, past, dtype, index, "d_state"),
+                                        Seq(*_seq(dx, wide, dtype, index, "dx")), dweight.data_ptr(), _at(dbias), dstate.data_ptr(),
+                                        _at(workspace), need, _stream(index))
     _check(rc, "sprnn_conv_backward")
     return dx, dweight, dbias, dstate
 
 
 # ------------------------------------------------------------------------------------------------------------------ norm
 
-def _norm(call, width, batch, steps, dtype, residual_dtype, eps, weight):
-    n = Norm(steps, batch, width, _type(dtype, "x"), _type(residual_dtype, "the residual"), float(eps))
-    if residual_dtype not in (dtype, call.torch.float32):
+def _norm(index, shape, dtype, stream_dtype, eps, weight):
+    if stream_dtype is not dtype and stream_dtype is not F32:
         raise TypeError("the residual must have the type of x or float32")
-    n.weight = call.plain(weight, (width,), call.torch.float32, "weight")
-    return n
+    return _NORM.pack(shape[0], shape[1], shape[2], _type(dtype, "x"), _type(stream_dtype, "the residual"), eps,
+                      _plain(weight, (shape[2],), F32, index, "weight"))
 
 
-def _norm_forward(x, weight, eps, residual, residual_out, y, y_type, scales):
-    call = _Call(x, "x")
+def _norm_forward(x, weight, eps, residual, residual_out, y, scales, quantized):
+    index = _index(x, "x")
     if x.dim() != 3:
         raise ValueError("x must be [T, B, W]")
-    shape = tuple(x.shape)
-    stream = x.dtype if residual is None else residual.dtype
-    n = _norm(call, shape[2], shape[1], shape[0], x.dtype, stream, eps, weight)
+    shape, dtype, device = x.shape, x.dtype, x.device
+    stream_dtype = dtype if residual is None else residual.dtype
+    norm = _norm(index, shape, dtype, stream_dtype, eps, weight)
+    y_dtype, blocks = E4M3 if quantized else dtype, (shape[0], shape[1], (shape[2] + 127) // 128)
     if residual_out is None and residual is not None:
-        residual_out = call.empty(shape, stream)
+        residual_out = torch.empty(shape, dtype=stream_dtype, device=device)
     if y is None:
-        y = call.empty(shape, call.torch.float8_e4m3fn if y_type == 3 else x.dtype)
-    blocks = (shape[0], shape[1], (shape[2] + 127) // 128)
-    if y_type == 3 and scales is None:
-        scales = call.empty(blocks, call.torch.float32)
-    rc = _library().sprnn_rms_norm(call.index, ctypes.byref(n), call.seq(x, shape, x.dtype, "x"), call.seq(residual, shape, stream, "residual"),
-                                   call.seq(residual_out, shape, stream, "residual_out"), n.type if y_type is None else y_type,
-                                   call.seq(y, shape, call.torch.float8_e4m3fn if y_type == 3 else x.dtype, "out"),
-                                   call.plain(scales, blocks, call.torch.float32, "scales") if y_type == 3 else None, call.stream())
+        y = torch.empty(shape, dtype=y_dtype, device=device)
+    if quantized and scales is None:
+        scales = torch.empty(blocks, dtype=F32, device=device)
+    rc = _library().sprnn_rms_norm(index, norm, Seq(*_seq(x, shape, dtype, index, "x")), Seq(*_seq(residual, shape, stream_dtype, index, "residual")),
+                                   Seq(*_seq(residual_out, shape, stream_dtype, index, "residual_out")), TYPES[y_dtype],
+                                   Seq(*_seq(y, shape, y_dtype, index, "out")), _plain(scales, blocks, F32, index, "scales"), _stream(index))
     _check(rc, "sprnn_rms_norm")
     return y, scales, residual_out
 
@@ -316,36 +307,34 @@ def _norm_forward(x, weight, eps, residual, residual_out, y, y_type, scales):
 def rms_norm(x, weight=None, eps=1e-5, residual=None, residual_out=None, out=None):
     """sprnn_rms_norm: x [T, B, W], residual [T, B, W] (the type of x, or float32) -> (y [T, B, W], x + residual), the
     second None without a residual (and without residual_out).  residual_out may be residual itself."""
-    y, _, r = _norm_forward(x, weight, eps, residual, residual_out, out, None, None)
+    y, _, r = _norm_forward(x, weight, eps, residual, residual_out, out, None, False)
     return y, r
 
 
 def rms_norm_fp8(x, weight=None, eps=1e-5, residual=None, residual_out=None, out=None, scales=None):
     """sprnn_rms_norm with its output in 8 bits: (y float8_e4m3fn [T, B, W], scales float32 [T, B, ceil(W / 128)],
     x + residual or None); y times the scale of its block of 128 is the normed row."""
-    return _norm_forward(x, weight, eps, residual, residual_out, out, 3, scales)
+    return _norm_forward(x, weight, eps, residual, residual_out, out, scales, True)
 
 
 def rms_norm_backward(dy, r, weight=None, eps=1e-5, d_residual=None, dr=None):
     """sprnn_rms_norm_backward: dy [T, B, W], the normed rows r [T, B, W] (x + residual, or x), d_residual (gradient of r
     from elsewhere) -> (gradient of r in the type of r, dweight [W] or None)."""
-    call = _Call(dy, "dy")
+    index = _index(dy, "dy")
     if dy.dim() != 3:
         raise ValueError("dy must be [T, B, W]")
-    shape = tuple(dy.shape)
-    if not isinstance(r, call.torch.Tensor):
+    if not isinstance(r, torch.Tensor):
         raise TypeError("r must be a CUDA tensor")
-    n = _norm(call, shape[2], shape[1], shape[0], dy.dtype, r.dtype, eps, weight)
-    need = ctypes.c_int64()
-    _check(_library().sprnn_rms_norm_sizes(ctypes.byref(n), ctypes.byref(need)), "sprnn_rms_norm_sizes")
-    workspace = call.workspace(need.value if weight is not None else 0)
+    shape, dtype, r_dtype, device = dy.shape, dy.dtype, r.dtype, dy.device
+    norm = _norm(index, shape, dtype, r_dtype, eps, weight)
+    need = 0 if weight is None else _sizes("sprnn_rms_norm_sizes", _NORM.pack(shape[0], shape[1], shape[2], 0, 0, 0.0, 0), 1)[0]
+    workspace = _workspace(need, device)
     if dr is None:
-        dr = call.empty(shape, r.dtype)
-    dweight = None if weight is None else call.empty((shape[2],), call.torch.float32)
-    rc = _library().sprnn_rms_norm_backward(call.index, ctypes.byref(n), call.seq(dy, shape, dy.dtype, "dy"), call.seq(r, shape, r.dtype, "r"),
-                                            call.seq(d_residual, shape, r.dtype, "d_residual"), call.seq(dr, shape, r.dtype, "dr"),
-                                            None if dweight is None else dweight.data_ptr(), workspace.data_ptr(), workspace.numel(),
-                                            call.stream())
+        dr = torch.empty(shape, dtype=r_dtype, device=device)
+    dweight = None if weight is None else torch.empty((shape[2],), dtype=F32, device=device)
+    rc = _library().sprnn_rms_norm_backward(index, norm, Seq(*_seq(dy, shape, dtype, index, "dy")), Seq(*_seq(r, shape, r_dtype, index, "r")),
+                                            Seq(*_seq(d_residual, shape, r_dtype, index, "d_residual")),
+                                            Seq(*_seq(dr, shape, r_dtype, index, "dr")), _at(dweight), _at(workspace), need, _stream(index))
     _check(rc, "sprnn_rms_norm_backward")
     return dr, dweight
 
@@ -356,22 +345,23 @@ def project_fp8(x, x_scales, w, w_scales, bias=None, dtype=None, out=None):
     """sprnn_project_quantized: x float8_e4m3fn [T, B, K] with x_scales [T, B, ceil(K / 128)] (as rms_norm_fp8 returns
     them), w float8_e4m3fn [R, K] with w_scales [ceil(R / 128), ceil(K / 128)], bias [R] -> [T, B, R] in dtype (float32
     unless said otherwise: the ``x`` argument of SparseRNN's forward calls)."""
-    call = _Call(x, "x")
-    f32, e4m3 = call.torch.float32, call.torch.float8_e4m3fn
-    if x.dim() != 3 or not isinstance(w, call.torch.Tensor) or w.dim() != 2:
+    index = _index(x, "x")
+    if x.dim() != 3 or not isinstance(w, torch.Tensor) or w.dim() != 2:
         raise ValueError("x must be [T, B, K] and w must be [R, K]")
-    T, batch, inputs = x.shape
+    if x_scales is None or w_scales is None:
+        raise TypeError("x_scales and w_scales must be float32 tensors on cuda:%d" % index)
+    shape = x.shape
+    T, batch, inputs = shape
     rows = w.shape[0]
-    p = Product(T, batch, rows, inputs)
     blocks = (inputs + 127) // 128
-    p.x, p.x_scales = call.seq(x, (T, batch, inputs), e4m3, "x"), call.plain(x_scales, (T, batch, blocks), f32, "x_scales")
-    p.w, p.w_scales = call.plain(w, (rows, inputs), e4m3, "w"), call.plain(w_scales, ((rows + 127) // 128, blocks), f32, "w_scales")
-    p.bias = call.plain(bias, (rows,), f32, "bias")
+    product = _PRODUCT.pack(T, batch, rows, inputs, *_seq(x, shape, E4M3, index, "x"), _plain(x_scales, (T, batch, blocks), F32, index, "x_scales"),
+                            _plain(w, (rows, inputs), E4M3, index, "w"),
+                            _plain(w_scales, ((rows + 127) // 128, blocks), F32, index, "w_scales"), _plain(bias, (rows,), F32, index, "bias"))
     if out is None:
-        out = call.empty((T, batch, rows), f32 if dtype is None else dtype)
+        out = torch.empty((T, batch, rows), dtype=F32 if dtype is None else dtype, device=x.device)
     elif dtype is not None and out.dtype != dtype:
-        raise TypeError("out must be a %s tensor" % str(dtype).replace("torch.", ""))
-    rc = _library().sprnn_project_quantized(call.index, ctypes.byref(p), _type(out.dtype, "out"), call.seq(out, (T, batch, rows), out.dtype, "out"),
-                                            call.stream())
+        raise TypeError("out must be a %s tensor" % _name(dtype))
+    rc = _library().sprnn_project_quantized(index, product, _type(out.dtype, "out"),
+                                            Seq(*_seq(out, (T, batch, rows), out.dtype, index, "out")), _stream(index))
     _check(rc, "sprnn_project_quantized")
     return out

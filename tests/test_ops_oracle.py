@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import ops_oracle as ref
+import ops_structures as st
 from paper_1804_10223_amd import binding, ops
 
 
@@ -86,13 +87,39 @@ def _seq(step=8, sample=8, at=AT):
     return ops.Seq(at, step, sample)
 
 
+def _own(s):
+    return st.Seq(s.data, s.step, s.sample)
+
+
 def _scan_arguments(**over):
-    s = ops.Scan(4, 1, 8, 4, 2, 0, 1)
-    s.u = s.dt = s.B = s.C = _seq()
+    s = st.Scan(4, 1, 8, 4, 2, 0, 1)
+    s.u = s.dt = s.B = s.C = _own(_seq())
     s.A = AT
     for k, v in over.items():
-        setattr(s, k, v)
+        setattr(s, k, _own(v) if isinstance(v, ops.Seq) else v)
     return s
+
+
+def test_the_packed_structures_are_those_of_the_header(tmp_path):
+    import os
+    import shutil
+    import subprocess
+    if shutil.which("gcc") is None:
+        pytest.skip("no gcc here")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    names = {"scan": (st.Scan, ops._SCAN), "scan_gradients": (st.ScanGradientBuffers, ops._SCAN_GRADIENTS), "conv": (st.Conv, ops._CONV),
+             "norm": (st.Norm, ops._NORM), "product": (st.Product, ops._PRODUCT)}
+    lines = ['printf("%%zu", sizeof(sprnn_%s_t));' % n + "".join(
+        'printf(" %%zu", offsetof(sprnn_%s_t, %s));' % (n, field) for field, _ in names[n][0]._fields_) + 'printf("\\n");' for n in names]
+    (tmp_path / "sizes.c").write_text("#include <stddef.h>\n#include <stdio.h>\n#include \"sprnn.h\"\nint main(void) {\n%s\nreturn 0;\n}\n" % "\n".join(lines))
+    exe = str(tmp_path / "sizes")
+    subprocess.run(["gcc", "-I" + os.path.join(root, "include"), str(tmp_path / "sizes.c"), "-o", exe], check=True)
+    said = subprocess.run([exe], check=True, capture_output=True, text=True).stdout.splitlines()
+    for (structure, packed), line in zip(names.values(), said):
+        size, *offsets = [int(x) for x in line.split()]
+        assert size == packed.size == ctypes.sizeof(structure)
+        assert offsets == [getattr(structure, field).offset for field, _ in structure._fields_]
+    assert ctypes.sizeof(ops.Seq) == ctypes.sizeof(st.Seq) == 24
 
 
 @pytest.mark.parametrize("over", [dict(steps=-1), dict(steps=(1 << 22) + 1), dict(batch=-1), dict(batch=65536), dict(channels=0),
@@ -104,7 +131,7 @@ def test_scan_refuses(over):
     lib = ops._library()
     s = _scan_arguments(**over)
     assert lib.sprnn_scan_forward(0, ctypes.byref(s), None, _seq(), None, None, None, 0, None) == binding.SPRNN_ERR_INVALID
-    g = ops.ScanGradientBuffers()
+    g = st.ScanGradientBuffers()
     assert lib.sprnn_scan_backward(0, ctypes.byref(s), _seq(), None, AT, ctypes.byref(g), AT, 1 << 40, None) == binding.SPRNN_ERR_INVALID
 
 
@@ -123,22 +150,22 @@ def test_scan_refuses_buffers():
     assert need > 0
     assert forward(s=long, work=AT, size=need - 1) == bad and forward(s=long, work=None, size=need) == bad
     assert forward(s=long, work=AT + 8, size=need) == bad
-    g = ops.ScanGradientBuffers()
+    g = st.ScanGradientBuffers()
     backward = lambda s=s, dy=_seq(), state=None, kept=AT, g=g, work=AT, size=1 << 40: lib.sprnn_scan_backward(
         0, ctypes.byref(s), dy, state, kept, ctypes.byref(g) if g is not None else None, work, size, None)
     assert backward(kept=None) == bad and backward(kept=AT + 4) == bad and backward(dy=_seq(at=None)) == bad and backward(g=None) == bad
     assert backward(work=None) == bad and backward(size=ops.scan_sizes(4, 1, 8, 4, 2)[1] - 1) == bad
-    assert backward(g=ops.ScanGradientBuffers(z=_seq())) == bad            # a gate's gradient without a gate
-    assert backward(g=ops.ScanGradientBuffers(u=_seq(step=4))) == bad
+    assert backward(g=st.ScanGradientBuffers(z=_own(_seq()))) == bad            # a gate's gradient without a gate
+    assert backward(g=st.ScanGradientBuffers(u=_own(_seq(step=4)))) == bad
     with pytest.raises(binding.SprnnError):
         ops.scan_sizes(1, 1, 7, 4, 2)
 
 
 def _conv_arguments(**over):
-    c = ops.Conv(4, 1, 8, 4, 0, 1)
-    c.x, c.weight = _seq(), AT
+    c = st.Conv(4, 1, 8, 4, 0, 1)
+    c.x, c.weight = _own(_seq()), AT
     for k, v in over.items():
-        setattr(c, k, v)
+        setattr(c, k, _own(v) if isinstance(v, ops.Seq) else v)
     return c
 
 
@@ -171,7 +198,7 @@ def test_conv_refuses_buffers():
                                   dict(eps=float("nan")), dict(weight=AT + 2)])
 def test_norm_refuses(over):
     lib, bad = ops._library(), binding.SPRNN_ERR_INVALID
-    n = ops.Norm(4, 1, 8, 1, 0, 1e-5)
+    n = st.Norm(4, 1, 8, 1, 0, 1e-5)
     for k, v in over.items():
         setattr(n, k, v)
     none = ops.Seq()
@@ -181,7 +208,7 @@ def test_norm_refuses(over):
 
 def test_norm_refuses_buffers():
     lib, bad, none = ops._library(), binding.SPRNN_ERR_INVALID, ops.Seq()
-    n = ops.Norm(4, 1, 8, 1, 0, 1e-5)
+    n = st.Norm(4, 1, 8, 1, 0, 1e-5)
     call = lambda x=_seq(), r=none, ro=none, t=1, y=_seq(), s=None: lib.sprnn_rms_norm(0, ctypes.byref(n), x, r, ro, t, y, s, None)
     assert call(x=none) == bad and call(y=none) == bad and call(t=0) == bad and call(t=2) == bad      # y in another type
     assert call(t=3) == bad and call(t=1, s=AT) == bad and call(t=3, s=AT + 2) == bad                 # scales with e4m3, and only then
@@ -198,13 +225,13 @@ def test_project_refuses():
     lib, bad = ops._library(), binding.SPRNN_ERR_INVALID
 
     def call(out_type=0, out=_seq(), **over):
-        p = ops.Product(4, 1, 8, 16)
-        p.x, p.x_scales, p.w, p.w_scales = _seq(16, 16), AT, AT, AT
+        p = st.Product(4, 1, 8, 16)
+        p.x, p.x_scales, p.w, p.w_scales = _own(_seq(16, 16)), AT, AT, AT
         for k, v in over.items():
             setattr(p, k, v)
         return lib.sprnn_project_quantized(0, ctypes.byref(p), out_type, out, None)
 
-    for over in (dict(steps=-1), dict(batch=70000), dict(rows=0), dict(inputs=0), dict(inputs=(1 << 24) + 1), dict(x=ops.Seq()),
+    for over in (dict(steps=-1), dict(batch=70000), dict(rows=0), dict(inputs=0), dict(inputs=(1 << 24) + 1), dict(x=st.Seq()),
                  dict(x_scales=None), dict(x_scales=AT + 2), dict(w=None), dict(w_scales=None), dict(w_scales=AT + 1), dict(bias=AT + 2)):
         assert call(**over) == bad, over
     assert call(out_type=3) == bad and call(out=_seq(step=7)) == bad and call(out=ops.Seq()) == bad
@@ -213,13 +240,13 @@ def test_project_refuses():
 
 def test_calls_without_work_succeed_without_a_gpu():
     lib, none = ops._library(), ops.Seq()
-    s = _scan_arguments(batch=0, u=none, dt=none, B=none, C=none)
+    s = _scan_arguments(batch=0, u=_own(none), dt=_own(none), B=_own(none), C=_own(none))
     assert lib.sprnn_scan_forward(0, ctypes.byref(s), None, none, None, None, None, 0, None) == 0
     c = _conv_arguments(batch=0, x=none)
     assert lib.sprnn_conv_forward(0, ctypes.byref(c), none, None, None) == 0
-    n = ops.Norm(0, 3, 8, 0, 0, 1e-5)
+    n = st.Norm(0, 3, 8, 0, 0, 1e-5)
     assert lib.sprnn_rms_norm(0, ctypes.byref(n), none, none, none, 0, none, None, None) == 0
-    p = ops.Product(0, 3, 8, 16)
+    p = st.Product(0, 3, 8, 16)
     assert lib.sprnn_project_quantized(0, ctypes.byref(p), 0, none, None) == 0
 
 
