@@ -170,12 +170,255 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, Elemen
   }
 }
 
+// Few rows of x: the weights are read once and bound the call.  A workgroup owns 16 rows of w and up to 16 MT rows of x, its
+// eight wavefronts share out the blocks of 128 inputs and fetch their fragments straight from memory, two blocks ahead; the
+// eight sums meet in LDS.  (8 x 2304 x 9216 on 128 x 128 tiles: 28 us, 72 workgroups.)
+constexpr int kFewWaves = 8;
+template <int TYPE, int MT>
+__global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(ProductArgs a, Element<TYPE>* out) {
+  constexpr bool kWide = TYPE == SPRNN_TYPE_F32;
+  __shared__ floatx4 sums[kFewWaves][MT][64];
+  const int lane = threadIdx.x & 63, fr = lane & 15, fq = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tiles_r = (a.rows + 15) / 16;
+  const int r0 = (int)(blockIdx.x % tiles_r) * 16;
+  const int64_t m0 = (int64_t)(blockIdx.x / tiles_r) * (16 * MT);
+  const uint8_t* const w_row = a.w + (int64_t)min(r0 + fr, a.rows - 1) * a.inputs;
+  const float* const w_scale = a.w_scales + (int64_t)(r0 / 128) * a.blocks;
+  const uint8_t* x_row[MT];
+  const float* scale_row[MT];
+#pragma unroll
+  for (int j = 0; j < MT; ++j) {
+    const int64_t m = min(m0 + j * 16 + fr, a.vectors - 1);
+    x_row[j] = a.x + (m / a.batch) * a.x_step + (m % a.batch) * a.x_sample;
+    scale_row[j] = a.x_scales + m * a.blocks;
+  }
+  struct Block {
+    uint4 w[2], x[MT][2];
+    float s[MT], ws;
+  };
+  auto fetch = [&](Block& f, int block) {
+    const int at = min(block, a.blocks - 1), k = at * kSlab + fq * 16;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) f.w[i] = load_piece(w_row, k + 64 * i, a.inputs);
+    f.ws = block < a.blocks ? w_scale[at] : 0.0f;
+#pragma unroll
+    for (int j = 0; j < MT; ++j) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) f.x[j][i] = load_piece(x_row[j], k + 64 * i, a.inputs);
+      f.s[j] = scale_row[j][at];
+    }
+  };
+  floatx4 acc[MT];
+#pragma unroll
+  for (int j = 0; j < MT; ++j) acc[j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  auto work = [&](const Block& f) {
+    const Fragment<kWide> wf(f.w[0], f.w[1]);
+#pragma unroll
+    for (int j = 0; j < MT; ++j) {
+      const floatx4 block = multiply(wf, Fragment<kWide>(f.x[j][0], f.x[j][1]));
+      const float s = f.s[j] * f.ws;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) acc[j][v] += block[v] * s;
+    }
+  };
+  for (int block = wave; block < a.blocks; block += 2 * kFewWaves) {
+    Block f[2];
+    fetch(f[0], block);
+    fetch(f[1], block + kFewWaves);
+    work(f[0]);
+    if (block + kFewWaves < a.blocks) work(f[1]);
+  }
+#pragma unroll
+  for (int j = 0; j < MT; ++j) sums[wave][j][lane] = acc[j];
+  __syncthreads();
+  const int r = r0 + fq * 4;
+  for (int j = wave; j < MT; j += kFewWaves) {
+    floatx4 sum = sums[0][j][lane];
+#pragma unroll
+    for (int w = 1; w < kFewWaves; ++w) sum += sums[w][j][lane];
+    const int64_t m = m0 + j * 16 + fr;
+    if (m >= a.vectors || r >= a.rows) continue;
+    store_four(out + (m / a.batch) * a.out_step + (m % a.batch) * a.out_sample, r, a.rows, sum, a.bias);
+  }
+}
+
+// Many rows: a wavefront multiplies 64 rows of x with 32 IR rows of w, WR x WM wavefronts are a workgroup.  Rows go from
+// memory into LDS without registers between (16 bytes a lane), a slab ahead of the one that is multiplied; the swizzle of
+// piece_at is in the addresses that the lanes fetch.  Instructions of 32 x 32 take half the issue slots of 16 x 16; the
+// vector unit needs them: with operands of 16 bits, 64 x 64 outputs of a slab are 1024 cycles of matrix instructions next to
+// 128 conversions and 64 scaled sums, and the sums, the widened fragments and the running sums fill the registers (IR = 4
+// is 27 too many).  On e4m3 itself the fragments are a quarter of that, and 128 x 64 outputs a wavefront halve what LDS
+// has to deliver a matrix instruction.
+template <bool WIDE> struct Many;
+template <> struct Many<true> { static constexpr int kIR = 2, kWR = 2, kWM = 2; };
+template <> struct Many<false> { static constexpr int kIR = 4, kWR = 2, kWM = 4; };
+template <bool WIDE> constexpr int many_r() { return Many<WIDE>::kWR * Many<WIDE>::kIR * 32; }
+template <bool WIDE> constexpr int many_m() { return Many<WIDE>::kWM * 64; }
+template <bool WIDE> constexpr int many_threads() { return Many<WIDE>::kWR * Many<WIDE>::kWM * 64; }
+template <bool WIDE> constexpr int many_stage() { return (many_r<WIDE>() + many_m<WIDE>()) * kSlab; }
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+
+// 32 rows x 128 inputs of a block: this lane's four pieces of 16.
+template <bool WIDE> struct Strip;
+template <> struct Strip<false> {
+  intx8 v[2];
+  __device__ __forceinline__ void set(int i, const uint4& p) {
+    intx8& to = v[i >> 1];
+    const int at = (i & 1) * 4;
+    to[at] = (int)p.x; to[at + 1] = (int)p.y; to[at + 2] = (int)p.z; to[at + 3] = (int)p.w;
+  }
+};
+template <> struct Strip<true> {
+  half8_t v[8];
+  __device__ __forceinline__ void set(int i, const uint4& p) {
+    v[2 * i] = Fragment<true>::widen(p.x, p.y);
+    v[2 * i + 1] = Fragment<true>::widen(p.z, p.w);
+  }
+};
+__device__ __forceinline__ floatx16 multiply(const Strip<false>& w, const Strip<false>& x) {
+  floatx16 c = {};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w.v[i], x.v[i], c, 0, 0, 0, 0, 0, 0);
+  return c;
+}
+__device__ __forceinline__ floatx16 multiply(const Strip<true>& w, const Strip<true>& x) {
+  floatx16 c = {};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_32x32x16_f16(w.v[i], x.v[i], c, 0, 0, 0);
+  return c;
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(many_threads<TYPE == SPRNN_TYPE_F32>(), 2) void product_many_kernel(ProductArgs a, Element<TYPE>* out) {
+  constexpr bool kWide = TYPE == SPRNN_TYPE_F32;
+  constexpr int IR = Many<kWide>::kIR, WR = Many<kWide>::kWR, kM = many_m<kWide>(), kR = many_r<kWide>();
+  constexpr int kWaves = many_threads<kWide>() / 64, kCopiesM = kM / (kWaves * 8), kCopiesR = kR / (kWaves * 8);
+  static_assert(kWaves * 8 % 16 == 0, "a lane fetches the same piece of all its rows");
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // Workgroups go to the eight XCDs in turn: each gets a run of tiles, eight along m by a few along r at a time, whose rows
+  // its L2 holds.
+  const int nb = gridDim.x, bid = blockIdx.x;
+  const int tiles_r = (a.rows + kR - 1) / kR;
+  const int id = nb % 8 == 0 ? (bid % 8) * (nb / 8) + bid / 8 : bid;
+  const int group = id / (8 * tiles_r), in_group = id - group * 8 * tiles_r, deep = min(8, a.tiles_m - group * 8);
+  const int64_t m0 = (int64_t)(group * 8 + in_group % deep) * kM;
+  const int r0 = in_group / deep * kR;
+
+  // this lane's part of the copies: rows (i * kWaves + wave) * 8 + lane / 8 of x and w, 16 bytes
+  const int own_row = wave * 8 + (lane >> 3), piece = ((lane & 7) ^ ((own_row >> 1) & 7)) * 16;
+  const uint8_t* x_at[kCopiesM];
+  const uint8_t* w_at[kCopiesR];
+#pragma unroll
+  for (int i = 0; i < kCopiesM; ++i) {
+    const int64_t m = min(m0 + i * kWaves * 8 + own_row, a.vectors - 1);
+    x_at[i] = a.x + (m / a.batch) * a.x_step + (m % a.batch) * a.x_sample + piece;
+  }
+#pragma unroll
+  for (int i = 0; i < kCopiesR; ++i) w_at[i] = a.w + (int64_t)min(r0 + i * kWaves * 8 + own_row, a.rows - 1) * a.inputs + piece;
+  auto bring = [&](const uint8_t* from, uint8_t* to, bool there) {
+    typedef const __attribute__((address_space(1))) void* Global;
+    typedef __attribute__((address_space(3))) void* Local;
+    if (there) __builtin_amdgcn_global_load_lds((Global)from, (Local)to, 16, 0, 0);
+    else *reinterpret_cast<uint4*>(to + lane * 16) = make_uint4(0, 0, 0, 0);
+  };
+  auto copy = [&](int slab, int at) {
+    uint8_t* const to = lds + at * many_stage<kWide>() + wave * 8 * kSlab;
+    const int k = slab * kSlab;
+    const bool there = k + piece < a.inputs;     // pieces are whole: the rows' length is a multiple of 16
+#pragma unroll
+    for (int i = 0; i < kCopiesM; ++i) bring(x_at[i] + k, to + i * kWaves * 8 * kSlab, there);
+#pragma unroll
+    for (int i = 0; i < kCopiesR; ++i) bring(w_at[i] + k, to + (kM + i * kWaves * 8) * kSlab, there);
+  };
+
+  const int wr = wave % WR * (IR * 32), wm = wave / WR * 64;
+  const int fr = lane & 31, half = lane >> 5;
+  const float* scale_row[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) scale_row[j] = a.x_scales + min(m0 + wm + j * 32 + fr, a.vectors - 1) * a.blocks;
+  const float* const w_scale = a.w_scales + (int64_t)min((r0 + wr) / 128, (a.rows - 1) / 128) * a.blocks;
+  floatx16 acc[IR][2];
+#pragma unroll
+  for (int i = 0; i < IR; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) acc[i][j] = floatx16{};
+
+  auto strip = [&](Strip<kWide>& f, const uint8_t* tile, int row) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f.set(i, *reinterpret_cast<const uint4*>(tile + piece_at(row, 2 * i + half)));
+  };
+  copy(0, 0);
+  float s[2] = {scale_row[0][0] * w_scale[0], scale_row[1][0] * w_scale[0]};
+  __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0): the copies have no register that the compiler would wait for
+  __syncthreads();
+  for (int slab = 0; slab < a.blocks; ++slab) {
+    const uint8_t* const xs = lds + (slab & 1) * many_stage<kWide>();
+    const uint8_t* const ws = xs + kM * kSlab;
+    const int next = min(slab + 1, a.blocks - 1);
+    if (slab + 1 < a.blocks) copy(slab + 1, (slab + 1) & 1);
+    const float s0 = scale_row[0][next] * w_scale[next], s1 = scale_row[1][next] * w_scale[next];
+    Strip<kWide> xf[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) strip(xf[j], xs, wm + j * 32 + fr);
+#pragma unroll
+    for (int i = 0; i < IR; ++i) {
+      Strip<kWide> wf;
+      strip(wf, ws, wr + i * 32 + fr);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const floatx16 block = multiply(wf, xf[j]);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[i][j][v] += block[v] * s[j];
+      }
+    }
+    s[0] = s0;
+    s[1] = s1;
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    __syncthreads();
+  }
+  // element v of lane (fr, half) of a 32 x 32 tile: row 8 (v / 4) + 4 half + v % 4 of w, row fr of x
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int64_t m = m0 + wm + j * 32 + fr;
+    if (m >= a.vectors) continue;
+    Element<TYPE>* const row = out + (m / a.batch) * a.out_step + (m % a.batch) * a.out_sample;
+#pragma unroll
+    for (int i = 0; i < IR; ++i) {
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int r = r0 + wr + i * 32 + v * 8 + half * 4;
+        if (r < a.rows) store_four(row, r, a.rows, floatx4{acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]}, a.bias);
+      }
+    }
+  }
+}
+
 template <int TYPE>
 hipError_t run_product(ProductArgs a, const sprnn_seq_t& out, hipStream_t stream) {
+  Element<TYPE>* const to = static_cast<Element<TYPE>*>(out.data);
+  auto groups = [&](int m, int r) { return (a.vectors + m - 1) / m * ((a.rows + r - 1) / r); };
+  if (a.vectors <= 64) {
+    const int64_t n = groups(a.vectors <= 16 ? 16 : a.vectors <= 32 ? 32 : 64, 16);
+    auto kernel = a.vectors <= 16 ? product_few_kernel<TYPE, 1> : a.vectors <= 32 ? product_few_kernel<TYPE, 2> : product_few_kernel<TYPE, 4>;
+    return launch(kernel, dim3((unsigned)n), dim3(64 * kFewWaves), 0, stream, a, to);
+  }
+  const bool aligned = a.inputs % 16 == 0 && aligned_to(a.x, 16) && aligned_to(a.w, 16) && a.x_step % 16 == 0 && a.x_sample % 16 == 0;
+  constexpr bool kWide = TYPE == SPRNN_TYPE_F32;
+  if (aligned && groups(many_m<kWide>(), many_r<kWide>()) >= 192) {
+    a.tiles_m = (int)((a.vectors + many_m<kWide>() - 1) / many_m<kWide>());
+    const int64_t n = groups(many_m<kWide>(), many_r<kWide>());
+    if (n > 0x7fffffffLL) return hipErrorInvalidValue;
+    const hipError_t e = hipFuncSetAttribute((const void*)product_many_kernel<TYPE>, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * many_stage<kWide>());
+    if (e != hipSuccess) return e;
+    return launch(product_many_kernel<TYPE>, dim3((unsigned)n), dim3(many_threads<kWide>()), 2 * many_stage<kWide>(), stream, a, to);
+  }
   a.tiles_m = (int)((a.vectors + kTileM - 1) / kTileM);
-  const int64_t tiles = (int64_t)a.tiles_m * ((a.rows + kTileR - 1) / kTileR);
+  const int64_t tiles = groups(kTileM, kTileR);
   if (tiles > 0x7fffffffLL) return hipErrorInvalidValue;
-  return launch(product_kernel<TYPE>, dim3((unsigned)tiles), dim3(kThreads), 0, stream, a, static_cast<Element<TYPE>*>(out.data));
+  return launch(product_kernel<TYPE>, dim3((unsigned)tiles), dim3(kThreads), 0, stream, a, to);
 }
 
 }  // namespace

@@ -411,6 +411,12 @@ PROJECTS = [
     (1, 16, 2304, 5760, "f32", True, "time"),
     (1, 17, 1000, 2310, "bf16", True, "time"),
     (1, 64, 1536, 1024, "f32", False, "time"),
+    # enough rows and outputs for the largest tiles: ragged edges, a last block of 16, 112 or all 128 inputs
+    (525, 4, 272, 2310, "f32", True, "time"),
+    (700, 3, 240, 1700, "f32", False, "batch"),
+    (875, 4, 144, 3601, "bf16", True, "time"),
+    (1000, 4, 128, 3073, "f16", True, "time"),
+    (450, 8, 368, 3400, "bf16", False, "batch"),
 ]
 
 
@@ -429,6 +435,11 @@ def test_project_fp8(T, B, K, R, type, bias, layout):
     out = ops.project_fp8(x, xs.view(T, B, -1).cuda(), w.cuda(), ws.cuda(), None if b is None else b.cuda(), dtype=dtype)
     # the sum of a block of 128 exact products, a scale of two, the sum over blocks, the bias
     n = min(K, 128) + 3 + -(-K // 128) + 2
+    # Outputs of 16 bits: the matrix instruction on e4m3 adds eight products at the scale of the largest of them and keeps 13
+    # bits below it (one large product and a small one: 2^-13 of it is added, 2^-14 is not), so each of the eight loses less
+    # than 2^-13 of the largest, which is at most the eight's sum of absolute values: 8 x 2^-13 = 2^-10 of that sum, 2^14 EPS.
+    if dtype != F32:
+        n += 2 ** 14
     _close(out, want, size, n, "out")
     wide = torch.full((T, B, R + 5), 7.0, dtype=dtype, device="cuda")
     ops.project_fp8(x, xs.view(T, B, -1).cuda(), w.cuda(), ws.cuda(), None if b is None else b.cuda(), out=wide[:, :, 3:3 + R])
