@@ -31,6 +31,7 @@ struct ProductArgs {
   const uint8_t* w;
   const float* w_scales;
   const float* bias;
+  bool x_even, out_even;               // row m of the view is m times its sample stride away
   int tiles_m;
 };
 
@@ -53,11 +54,33 @@ __device__ __forceinline__ uint4 load_piece(const uint8_t* row, int k, int input
 // bits, so that the sixteen rows that an LDS cycle serves are in sixteen different groups of banks.
 __device__ __forceinline__ int piece_at(int row, int q) { return row * kSlab + ((q ^ ((row >> 1) & 7)) << 4); }
 
+// Rows of a [T][B] view by their number t B + b: where the strides allow it (even), one multiplication.
+__device__ __forceinline__ int64_t row_offset(int64_t m, int batch, int64_t step, int64_t sample, bool even) {
+  if (even) return m * sample;
+  const uint32_t t = (uint32_t)m / (uint32_t)batch, b = (uint32_t)m - t * (uint32_t)batch;   // T B is below 2^31
+  return (int64_t)t * step + (int64_t)b * sample;
+}
+__device__ __forceinline__ const uint8_t* x_row_at(const ProductArgs& a, int64_t m) { return a.x + row_offset(m, a.batch, a.x_step, a.x_sample, a.x_even); }
+
+// Four neighbouring outputs of a row; their biases, zeros without any.
+__device__ __forceinline__ floatx4 bias_of(const float* bias, int r, int rows) {
+  floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (!bias) return v;
+  if (r + 4 <= rows) {
+    const Pack<float, 4> p = load_pack<4>(bias + r);
+    v = floatx4{p.v[0], p.v[1], p.v[2], p.v[3]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (r + i < rows) v[i] = bias[r + i];
+  }
+  return v;
+}
 template <typename E>
-__device__ __forceinline__ void store_four(E* row, int r, int rows, const floatx4& v, const float* bias) {
+__device__ __forceinline__ void store_four(E* row, int r, int rows, const floatx4& v) {
   Pack<E, 4> p;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) p.v[i] = (E)(v[i] + (bias && r + i < rows ? bias[r + i] : 0.0f));
+  for (int i = 0; i < 4; ++i) p.v[i] = (E)v[i];
   if (r + 4 <= rows) store_pack(row + r, p);
   else store_part(row + r, p, rows - r);
 }
@@ -103,7 +126,7 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, Elemen
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int64_t m = min(m0 + (tid >> 3) + 32 * i, a.vectors - 1);
-    x_row[i] = a.x + (m / a.batch) * a.x_step + (m % a.batch) * a.x_sample;
+    x_row[i] = x_row_at(a, m);
     w_row[i] = a.w + (int64_t)min(r0 + (tid >> 3) + 32 * i, a.rows - 1) * a.inputs;
   }
   const float* const scale_row = a.x_scales + min(m0 + (tid & (kTileM - 1)), a.vectors - 1) * a.blocks;
@@ -158,14 +181,14 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, Elemen
     }
   }
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int64_t m = m0 + wm + j * 16 + fr;
-    if (m >= a.vectors) continue;
-    Element<TYPE>* const row = out + (m / a.batch) * a.out_step + (m % a.batch) * a.out_sample;
+  for (int i = 0; i < 4; ++i) {
+    const int r = r0 + wr + i * 16 + fq * 4;
+    if (r >= a.rows) break;
+    const floatx4 bias = bias_of(a.bias, r, a.rows);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = r0 + wr + i * 16 + fq * 4;
-      if (r < a.rows) store_four(row, r, a.rows, acc[i][j], a.bias);
+    for (int j = 0; j < 4; ++j) {
+      const int64_t m = m0 + wm + j * 16 + fr;
+      if (m < a.vectors) store_four(out + row_offset(m, a.batch, a.out_step, a.out_sample, a.out_even), r, a.rows, acc[i][j] + bias);
     }
   }
 }
@@ -190,7 +213,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(ProductArgs
 #pragma unroll
   for (int j = 0; j < MT; ++j) {
     const int64_t m = min(m0 + j * 16 + fr, a.vectors - 1);
-    x_row[j] = a.x + (m / a.batch) * a.x_step + (m % a.batch) * a.x_sample;
+    x_row[j] = x_row_at(a, m);
     scale_row[j] = a.x_scales + m * a.blocks;
   }
   struct Block {
@@ -239,7 +262,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(ProductArgs
     for (int w = 1; w < kFewWaves; ++w) sum += sums[w][j][lane];
     const int64_t m = m0 + j * 16 + fr;
     if (m >= a.vectors || r >= a.rows) continue;
-    store_four(out + (m / a.batch) * a.out_step + (m % a.batch) * a.out_sample, r, a.rows, sum, a.bias);
+    store_four(out + row_offset(m, a.batch, a.out_step, a.out_sample, a.out_even), r, a.rows, sum + bias_of(a.bias, r, a.rows));
   }
 }
 
@@ -314,7 +337,7 @@ __global__ __launch_bounds__(many_threads<TYPE == SPRNN_TYPE_F32>(), 2) void pro
 #pragma unroll
   for (int i = 0; i < kCopiesM; ++i) {
     const int64_t m = min(m0 + i * kWaves * 8 + own_row, a.vectors - 1);
-    x_at[i] = a.x + (m / a.batch) * a.x_step + (m % a.batch) * a.x_sample + piece;
+    x_at[i] = x_row_at(a, m) + piece;
   }
 #pragma unroll
   for (int i = 0; i < kCopiesR; ++i) w_at[i] = a.w + (int64_t)min(r0 + i * kWaves * 8 + own_row, a.rows - 1) * a.inputs + piece;
@@ -380,17 +403,21 @@ __global__ __launch_bounds__(many_threads<TYPE == SPRNN_TYPE_F32>(), 2) void pro
     __syncthreads();
   }
   // element v of lane (fr, half) of a 32 x 32 tile: row 8 (v / 4) + 4 half + v % 4 of w, row fr of x
+  Element<TYPE>* row[2];
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int64_t m = m0 + wm + j * 32 + fr;
-    if (m >= a.vectors) continue;
-    Element<TYPE>* const row = out + (m / a.batch) * a.out_step + (m % a.batch) * a.out_sample;
+  for (int j = 0; j < 2; ++j)
+    row[j] = out + row_offset(min(m0 + wm + j * 32 + fr, a.vectors - 1), a.batch, a.out_step, a.out_sample, a.out_even);
 #pragma unroll
-    for (int i = 0; i < IR; ++i) {
+  for (int i = 0; i < IR; ++i) {
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const int r = r0 + wr + i * 32 + v * 8 + half * 4;
-        if (r < a.rows) store_four(row, r, a.rows, floatx4{acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]}, a.bias);
+    for (int v = 0; v < 4; ++v) {
+      const int r = r0 + wr + i * 32 + v * 8 + half * 4;
+      if (r >= a.rows) continue;
+      const floatx4 bias = bias_of(a.bias, r, a.rows);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const floatx4 sum = {acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]};
+        if (m0 + wm + j * 32 + fr < a.vectors) store_four(row[j], r, a.rows, sum + bias);
       }
     }
   }
@@ -436,7 +463,7 @@ extern "C" int sprnn_project_quantized(int device_id, const sprnn_product_t* p, 
   DeviceGuard guard(device_id);
   if (!guard.ok) return SPRNN_ERR_HIP;
   const ProductArgs a{(int64_t)p->steps * p->batch, p->batch, p->rows, p->inputs, (p->inputs + 127) / 128, p->x.step, p->x.sample, out.step, out.sample,
-                      static_cast<const uint8_t*>(p->x.data), p->x_scales, static_cast<const uint8_t*>(p->w), p->w_scales, p->bias, 0};
+                      static_cast<const uint8_t*>(p->x.data), p->x_scales, static_cast<const uint8_t*>(p->w), p->w_scales, p->bias, p->steps == 1 || p->x.step == p->batch * p->x.sample, p->steps == 1 || out.step == p->batch * out.sample, 0};
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const hipError_t e = out_type == SPRNN_TYPE_F32 ? run_product<SPRNN_TYPE_F32>(a, out, s) : out_type == SPRNN_TYPE_F16 ? run_product<SPRNN_TYPE_F16>(a, out, s)
                                                                                           : run_product<SPRNN_TYPE_BF16>(a, out, s);
