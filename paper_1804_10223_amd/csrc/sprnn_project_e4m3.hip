@@ -402,23 +402,40 @@ __global__ __launch_bounds__(many_threads<TYPE == SPRNN_TYPE_F32>(), 2) void pro
     __builtin_amdgcn_s_waitcnt(0x0f70);
     __syncthreads();
   }
-  // element v of lane (fr, half) of a 32 x 32 tile: row 8 (v / 4) + 4 half + v % 4 of w, row fr of x
-  Element<TYPE>* row[2];
+  // Sums leave through LDS: a lane has four neighbouring outputs of a row, 32 bytes of it a store with its neighbour.  A
+  // wavefront turns its own tiles, 32 rows of x by 64 of w at a time, and stores rows of 64 outputs.
+  constexpr int kPitch = 64 + 4;                 // floats; four more keep the rows of a turn off each other's banks
+  static_assert(kWaves * 32 * kPitch * 4 <= 2 * many_stage<kWide>(), "a turn of every wavefront fits");
+  float* const turn = reinterpret_cast<float*>(lds) + wave * 32 * kPitch;
+  auto in_order = [] {                           // LDS serves a wavefront in order; the compiler is to keep it
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
-    row[j] = out + row_offset(min(m0 + wm + j * 32 + fr, a.vectors - 1), a.batch, a.out_step, a.out_sample, a.out_even);
+  for (int pair = 0; pair < IR / 2; ++pair) {
+    const int r = r0 + wr + pair * 64 + (lane & 15) * 4;
+    const floatx4 bias = r < a.rows ? bias_of(a.bias, r, a.rows) : floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-  for (int i = 0; i < IR; ++i) {
+    for (int j = 0; j < 2; ++j) {
+      // element v of lane (fr, half) of a 32 x 32 tile: row 8 (v / 4) + 4 half + v % 4 of w, row fr of x
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      const int r = r0 + wr + i * 32 + v * 8 + half * 4;
-      if (r >= a.rows) continue;
-      const floatx4 bias = bias_of(a.bias, r, a.rows);
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const floatx4 sum = {acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]};
-        if (m0 + wm + j * 32 + fr < a.vectors) store_four(row[j], r, a.rows, sum + bias);
+        for (int v = 0; v < 4; ++v) {
+          const floatx16& t = acc[2 * pair + i][j];
+          *reinterpret_cast<floatx4*>(turn + fr * kPitch + i * 32 + v * 8 + half * 4) = floatx4{t[4 * v], t[4 * v + 1], t[4 * v + 2], t[4 * v + 3]};
+        }
+      in_order();
+#pragma unroll
+      for (int q = 0; q < 32; q += 4) {
+        const int row = q + (lane >> 4);
+        const int64_t m = m0 + wm + j * 32 + row;
+        const floatx4 sum = *reinterpret_cast<const floatx4*>(turn + row * kPitch + (lane & 15) * 4);
+        if (m < a.vectors && r < a.rows)
+          store_four(out + row_offset(m, a.batch, a.out_step, a.out_sample, a.out_even), r, a.rows, sum + bias);
       }
+      in_order();
     }
   }
 }
