@@ -268,11 +268,14 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(ProductArgs
 
 // Many rows: a wavefront multiplies 64 rows of x with 32 IR rows of w, WR x WM wavefronts are a workgroup.  Rows go from
 // memory into LDS without registers between (16 bytes a lane), a slab ahead of the one that is multiplied; the swizzle of
-// piece_at is in the addresses that the lanes fetch.  Instructions of 32 x 32 take half the issue slots of 16 x 16; the
+// piece_at is in the addresses that the lanes fetch.  Instructions of 32 x 32 take half the issue slots of 16 x 16, and the
 // vector unit needs them: with operands of 16 bits, 64 x 64 outputs of a slab are 1024 cycles of matrix instructions next to
-// 128 conversions and 64 scaled sums, and the sums, the widened fragments and the running sums fill the registers (IR = 4
-// is 27 too many).  On e4m3 itself the fragments are a quarter of that, and 128 x 64 outputs a wavefront halve what LDS
-// has to deliver a matrix instruction.
+// 128 conversions (5 cycles) and 64 scaled sums; the widened fragments and the running sums fill the registers (IR = 4 is 27
+// too many).  On e4m3 itself the fragments are a quarter of that, and 128 x 64 outputs a wavefront halve what LDS has to
+// deliver for a matrix instruction.
+// Measured on 8192 x 2304 x 9216: float32 430 us (matrix instructions 139 us of it at 2.4 GHz; the chip runs at 2.0 here),
+// bfloat16 220.  Of the float32 form, others came out within 5 % (eight wavefronts and three stages 425, half slabs in five
+// stages 470), and widening once a workgroup, on the way into LDS, at 500: twice the bytes through LDS.
 template <bool WIDE> struct Many;
 template <> struct Many<true> { static constexpr int kIR = 2, kWR = 2, kWM = 2; };
 template <> struct Many<false> { static constexpr int kIR = 4, kWR = 2, kWM = 4; };
@@ -280,9 +283,10 @@ template <bool WIDE> constexpr int many_r() { return Many<WIDE>::kWR * Many<WIDE
 template <bool WIDE> constexpr int many_m() { return Many<WIDE>::kWM * 64; }
 template <bool WIDE> constexpr int many_threads() { return Many<WIDE>::kWR * Many<WIDE>::kWM * 64; }
 template <bool WIDE> constexpr int many_stage() { return (many_r<WIDE>() + many_m<WIDE>()) * kSlab; }
+__device__ __attribute__((aligned(16))) const uint8_t nothing[16] = {};   // what pieces behind a row's end are copied from
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
-// 32 rows x 128 inputs of a block: this lane's four pieces of 16.
+// 32 rows of a slab: this lane's four pieces, every other one of its row.
 template <bool WIDE> struct Strip;
 template <> struct Strip<false> {
   intx8 v[2];
@@ -341,20 +345,27 @@ __global__ __launch_bounds__(many_threads<TYPE == SPRNN_TYPE_F32>(), 2) void pro
   }
 #pragma unroll
   for (int i = 0; i < kCopiesR; ++i) w_at[i] = a.w + (int64_t)min(r0 + i * kWaves * 8 + own_row, a.rows - 1) * a.inputs + piece;
-  auto bring = [&](const uint8_t* from, uint8_t* to, bool there) {
+  auto bring = [&](const uint8_t* from, uint8_t* to) {
     typedef const __attribute__((address_space(1))) void* Global;
     typedef __attribute__((address_space(3))) void* Local;
-    if (there) __builtin_amdgcn_global_load_lds((Global)from, (Local)to, 16, 0, 0);
-    else *reinterpret_cast<uint4*>(to + lane * 16) = make_uint4(0, 0, 0, 0);
+    __builtin_amdgcn_global_load_lds((Global)from, (Local)to, 16, 0, 0);
   };
   auto copy = [&](int slab, int at) {
     uint8_t* const to = lds + at * many_stage<kWide>() + wave * 8 * kSlab;
-    const int k = slab * kSlab;
+    const int64_t k = (int64_t)slab * kSlab;
     const bool there = k + piece < a.inputs;     // pieces are whole: the rows' length is a multiple of 16
 #pragma unroll
-    for (int i = 0; i < kCopiesM; ++i) bring(x_at[i] + k, to + i * kWaves * 8 * kSlab, there);
+    for (int i = 0; i < kCopiesM; ++i) bring(there ? x_at[i] + k : nothing, to + i * kWaves * 8 * kSlab);
 #pragma unroll
-    for (int i = 0; i < kCopiesR; ++i) bring(w_at[i] + k, to + (kM + i * kWaves * 8) * kSlab, there);
+    for (int i = 0; i < kCopiesR; ++i) bring(there ? w_at[i] + k : nothing, to + (kM + i * kWaves * 8) * kSlab);
+  };
+  // The copies have no registers that the compiler would wait for: every wavefront waits for its own, and for its reads of
+  // the slab that the next copies replace.
+  auto next_slab = [&] {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);          // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
   };
 
   const int wr = wave % WR * (IR * 32), wm = wave / WR * 64;
@@ -373,16 +384,15 @@ __global__ __launch_bounds__(many_threads<TYPE == SPRNN_TYPE_F32>(), 2) void pro
 #pragma unroll
     for (int i = 0; i < 4; ++i) f.set(i, *reinterpret_cast<const uint4*>(tile + piece_at(row, 2 * i + half)));
   };
-  copy(0, 0);
   float s[2] = {scale_row[0][0] * w_scale[0], scale_row[1][0] * w_scale[0]};
-  __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0): the copies have no register that the compiler would wait for
-  __syncthreads();
+  copy(0, 0);
+  next_slab();
   for (int slab = 0; slab < a.blocks; ++slab) {
     const uint8_t* const xs = lds + (slab & 1) * many_stage<kWide>();
     const uint8_t* const ws = xs + kM * kSlab;
     const int next = min(slab + 1, a.blocks - 1);
-    if (slab + 1 < a.blocks) copy(slab + 1, (slab + 1) & 1);
-    const float s0 = scale_row[0][next] * w_scale[next], s1 = scale_row[1][next] * w_scale[next];
+    const float s0 = scale_row[0][next], s1 = scale_row[1][next], w0 = w_scale[next];
+    copy(slab + 1, (slab + 1) & 1);              // (zeros behind the last one)
     Strip<kWide> xf[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) strip(xf[j], xs, wm + j * 32 + fr);
@@ -397,10 +407,9 @@ __global__ __launch_bounds__(many_threads<TYPE == SPRNN_TYPE_F32>(), 2) void pro
         for (int v = 0; v < 16; ++v) acc[i][j][v] += block[v] * s[j];
       }
     }
-    s[0] = s0;
-    s[1] = s1;
-    __builtin_amdgcn_s_waitcnt(0x0f70);
-    __syncthreads();
+    next_slab();
+    s[0] = s0 * w0;
+    s[1] = s1 * w0;
   }
   // Sums leave through LDS: a lane has four neighbouring outputs of a row, 32 bytes of it a store with its neighbour.  A
   // wavefront turns its own tiles, 32 rows of x by 64 of w at a time, and stores rows of 64 outputs.
