@@ -276,13 +276,13 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(ProductArgs
 // Measured on 8192 x 2304 x 9216: float32 430 us (matrix instructions 139 us of it at 2.4 GHz; the chip runs at 2.0 here),
 // bfloat16 220.  Of the float32 form, others came out within 5 % (eight wavefronts and three stages 425, half slabs in five
 // stages 470), and widening once a workgroup, on the way into LDS, at 500: twice the bytes through LDS.
-template <bool WIDE> struct Many;
-template <> struct Many<true> { static constexpr int kIR = 2, kWR = 2, kWM = 2; };
-template <> struct Many<false> { static constexpr int kIR = 4, kWR = 2, kWM = 4; };
-template <bool WIDE> constexpr int many_r() { return Many<WIDE>::kWR * Many<WIDE>::kIR * 32; }
-template <bool WIDE> constexpr int many_m() { return Many<WIDE>::kWM * 64; }
-template <bool WIDE> constexpr int many_threads() { return Many<WIDE>::kWR * Many<WIDE>::kWM * 64; }
-template <bool WIDE> constexpr int many_stage() { return (many_r<WIDE>() + many_m<WIDE>()) * kSlab; }
+template <int IR> struct Many;
+template <> struct Many<2> { static constexpr int kWR = 2, kWM = 2; };
+template <> struct Many<4> { static constexpr int kWR = 2, kWM = 4; };
+template <int IR> constexpr int many_r() { return Many<IR>::kWR * IR * 32; }
+template <int IR> constexpr int many_m() { return Many<IR>::kWM * 64; }
+template <int IR> constexpr int many_threads() { return Many<IR>::kWR * Many<IR>::kWM * 64; }
+template <int IR> constexpr int many_stage() { return (many_r<IR>() + many_m<IR>()) * kSlab; }
 __device__ __attribute__((aligned(16))) const uint8_t nothing[16] = {};   // what pieces behind a row's end are copied from
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
@@ -316,11 +316,11 @@ __device__ __forceinline__ floatx16 multiply(const Strip<true>& w, const Strip<t
   return c;
 }
 
-template <int TYPE>
-__global__ __launch_bounds__(many_threads<TYPE == SPRNN_TYPE_F32>(), 2) void product_many_kernel(ProductArgs a, Element<TYPE>* out) {
+template <int TYPE, int IR>
+__global__ __launch_bounds__(many_threads<IR>(), 2) void product_many_kernel(ProductArgs a, Element<TYPE>* out) {
   constexpr bool kWide = TYPE == SPRNN_TYPE_F32;
-  constexpr int IR = Many<kWide>::kIR, WR = Many<kWide>::kWR, kM = many_m<kWide>(), kR = many_r<kWide>();
-  constexpr int kWaves = many_threads<kWide>() / 64, kCopiesM = kM / (kWaves * 8), kCopiesR = kR / (kWaves * 8);
+  constexpr int WR = Many<IR>::kWR, kM = many_m<IR>(), kR = many_r<IR>();
+  constexpr int kWaves = many_threads<IR>() / 64, kCopiesM = kM / (kWaves * 8), kCopiesR = kR / (kWaves * 8);
   static_assert(kWaves * 8 % 16 == 0, "a lane fetches the same piece of all its rows");
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -351,7 +351,7 @@ __global__ __launch_bounds__(many_threads<TYPE == SPRNN_TYPE_F32>(), 2) void pro
     __builtin_amdgcn_global_load_lds((Global)from, (Local)to, 16, 0, 0);
   };
   auto copy = [&](int slab, int at) {
-    uint8_t* const to = lds + at * many_stage<kWide>() + wave * 8 * kSlab;
+    uint8_t* const to = lds + at * many_stage<IR>() + wave * 8 * kSlab;
     const int64_t k = (int64_t)slab * kSlab;
     const bool there = k + piece < a.inputs;     // pieces are whole: the rows' length is a multiple of 16
 #pragma unroll
@@ -388,7 +388,7 @@ __global__ __launch_bounds__(many_threads<TYPE == SPRNN_TYPE_F32>(), 2) void pro
   copy(0, 0);
   next_slab();
   for (int slab = 0; slab < a.blocks; ++slab) {
-    const uint8_t* const xs = lds + (slab & 1) * many_stage<kWide>();
+    const uint8_t* const xs = lds + (slab & 1) * many_stage<IR>();
     const uint8_t* const ws = xs + kM * kSlab;
     const int next = min(slab + 1, a.blocks - 1);
     const float s0 = scale_row[0][next], s1 = scale_row[1][next], w0 = w_scale[next];
@@ -414,7 +414,7 @@ __global__ __launch_bounds__(many_threads<TYPE == SPRNN_TYPE_F32>(), 2) void pro
   // Sums leave through LDS: a lane has four neighbouring outputs of a row, 32 bytes of it a store with its neighbour.  A
   // wavefront turns its own tiles, 32 rows of x by 64 of w at a time, and stores rows of 64 outputs.
   constexpr int kPitch = 64 + 4;                 // floats; four more keep the rows of a turn off each other's banks
-  static_assert(kWaves * 32 * kPitch * 4 <= 2 * many_stage<kWide>(), "a turn of every wavefront fits");
+  static_assert(kWaves * 32 * kPitch * 4 <= 2 * many_stage<IR>(), "a turn of every wavefront fits");
   float* const turn = reinterpret_cast<float*>(lds) + wave * 32 * kPitch;
   auto in_order = [] {                           // LDS serves a wavefront in order; the compiler is to keep it
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -453,20 +453,27 @@ template <int TYPE>
 hipError_t run_product(ProductArgs a, const sprnn_seq_t& out, hipStream_t stream) {
   Element<TYPE>* const to = static_cast<Element<TYPE>*>(out.data);
   auto groups = [&](int m, int r) { return (a.vectors + m - 1) / m * ((a.rows + r - 1) / r); };
-  if (a.vectors <= 64) {
-    const int64_t n = groups(a.vectors <= 16 ? 16 : a.vectors <= 32 ? 32 : 64, 16);
-    auto kernel = a.vectors <= 16 ? product_few_kernel<TYPE, 1> : a.vectors <= 32 ? product_few_kernel<TYPE, 2> : product_few_kernel<TYPE, 4>;
-    return launch(kernel, dim3((unsigned)n), dim3(64 * kFewWaves), 0, stream, a, to);
+  // Few rows, or outputs of fewer 128 x 128 tiles than half of the CUs.
+  if (a.vectors <= 64 || groups(kTileM, kTileR) < 128) {
+    const int rows = a.vectors <= 16 ? 16 : a.vectors <= 32 ? 32 : 64;
+    auto kernel = rows == 16 ? product_few_kernel<TYPE, 1> : rows == 32 ? product_few_kernel<TYPE, 2> : product_few_kernel<TYPE, 4>;
+    return launch(kernel, dim3((unsigned)groups(rows, 16)), dim3(64 * kFewWaves), 0, stream, a, to);
   }
-  const bool aligned = a.inputs % 16 == 0 && aligned_to(a.x, 16) && aligned_to(a.w, 16) && a.x_step % 16 == 0 && a.x_sample % 16 == 0;
-  constexpr bool kWide = TYPE == SPRNN_TYPE_F32;
-  if (aligned && groups(many_m<kWide>(), many_r<kWide>()) >= 192) {
-    a.tiles_m = (int)((a.vectors + many_m<kWide>() - 1) / many_m<kWide>());
-    const int64_t n = groups(many_m<kWide>(), many_r<kWide>());
-    if (n > 0x7fffffffLL) return hipErrorInvalidValue;
-    const hipError_t e = hipFuncSetAttribute((const void*)product_many_kernel<TYPE>, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * many_stage<kWide>());
-    if (e != hipSuccess) return e;
-    return launch(product_many_kernel<TYPE>, dim3((unsigned)n), dim3(many_threads<kWide>()), 2 * many_stage<kWide>(), stream, a, to);
+  // Copies of 16 bytes need rows that begin and end at multiples of them.
+  if (a.inputs % 16 == 0 && aligned_to(a.x, 16) && aligned_to(a.w, 16) && a.x_step % 16 == 0 && a.x_sample % 16 == 0) {
+    auto run = [&](auto kernel, int m, int r, int threads, int lds) {
+      a.tiles_m = (int)((a.vectors + m - 1) / m);
+      const int64_t n = groups(m, r);
+      if (n > 0x7fffffffLL) return hipErrorInvalidValue;
+      const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+      if (e != hipSuccess) return e;
+      return launch(kernel, dim3((unsigned)n), dim3((unsigned)threads), lds, stream, a, to);
+    };
+    if constexpr (TYPE != SPRNN_TYPE_F32) {
+      if (groups(many_m<4>(), many_r<4>()) >= 192)
+        return run(product_many_kernel<TYPE, 4>, many_m<4>(), many_r<4>(), many_threads<4>(), 2 * many_stage<4>());
+    }
+    return run(product_many_kernel<TYPE, 2>, many_m<2>(), many_r<2>(), many_threads<2>(), 2 * many_stage<2>());
   }
   a.tiles_m = (int)((a.vectors + kTileM - 1) / kTileM);
   const int64_t tiles = groups(kTileM, kTileR);
