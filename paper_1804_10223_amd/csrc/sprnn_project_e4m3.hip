@@ -193,20 +193,23 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, Elemen
   }
 }
 
-// Few rows of x: the weights are read once and bound the call.  A workgroup owns 16 rows of w and up to 16 MT rows of x, its
-// eight wavefronts share out the blocks of 128 inputs and fetch their fragments straight from memory, two blocks ahead; the
-// eight sums meet in LDS.  (8 x 2304 x 9216 on 128 x 128 tiles: 28 us, 72 workgroups.)
+// Few rows of x: the weights are read once and bound the call.  A workgroup owns 16 RT rows of w and up to 16 MT rows of x,
+// its eight wavefronts share out the blocks of 128 inputs and fetch their fragments straight from memory, two blocks ahead;
+// the eight sums meet in LDS.  (8 x 2304 x 9216 on 128 x 128 tiles: 28 us, 72 workgroups; here 9.  RT = 2 halves how often
+// many rows of x are fetched.)
 constexpr int kFewWaves = 8;
-template <int TYPE, int MT>
+template <int TYPE, int MT, int RT>
 __global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(ProductArgs a, Element<TYPE>* out) {
   constexpr bool kWide = TYPE == SPRNN_TYPE_F32;
-  __shared__ floatx4 sums[kFewWaves][MT][64];
+  __shared__ floatx4 sums[kFewWaves][RT * MT][64];
   const int lane = threadIdx.x & 63, fr = lane & 15, fq = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int tiles_r = (a.rows + 15) / 16;
-  const int r0 = (int)(blockIdx.x % tiles_r) * 16;
+  const int tiles_r = (a.rows + 16 * RT - 1) / (16 * RT);
+  const int r0 = (int)(blockIdx.x % tiles_r) * (16 * RT);
   const int64_t m0 = (int64_t)(blockIdx.x / tiles_r) * (16 * MT);
-  const uint8_t* const w_row = a.w + (int64_t)min(r0 + fr, a.rows - 1) * a.inputs;
+  const uint8_t* w_row[RT];
+#pragma unroll
+  for (int i = 0; i < RT; ++i) w_row[i] = a.w + (int64_t)min(r0 + i * 16 + fr, a.rows - 1) * a.inputs;
   const float* const w_scale = a.w_scales + (int64_t)(r0 / 128) * a.blocks;
   const uint8_t* x_row[MT];
   const float* scale_row[MT];
@@ -217,32 +220,39 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(ProductArgs
     scale_row[j] = a.x_scales + m * a.blocks;
   }
   struct Block {
-    uint4 w[2], x[MT][2];
+    uint4 w[RT][2], x[MT][2];
     float s[MT], ws;
   };
   auto fetch = [&](Block& f, int block) {
     const int at = min(block, a.blocks - 1), k = at * kSlab + fq * 16;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) f.w[i] = load_piece(w_row, k + 64 * i, a.inputs);
-    f.ws = block < a.blocks ? w_scale[at] : 0.0f;
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) f.w[i][h] = load_piece(w_row[i], k + 64 * h, a.inputs);
+    f.ws = w_scale[at];
 #pragma unroll
     for (int j = 0; j < MT; ++j) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) f.x[j][i] = load_piece(x_row[j], k + 64 * i, a.inputs);
+      for (int h = 0; h < 2; ++h) f.x[j][h] = load_piece(x_row[j], k + 64 * h, a.inputs);
       f.s[j] = scale_row[j][at];
     }
   };
-  floatx4 acc[MT];
+  floatx4 acc[RT][MT];
 #pragma unroll
-  for (int j = 0; j < MT; ++j) acc[j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
   auto work = [&](const Block& f) {
-    const Fragment<kWide> wf(f.w[0], f.w[1]);
 #pragma unroll
     for (int j = 0; j < MT; ++j) {
-      const floatx4 block = multiply(wf, Fragment<kWide>(f.x[j][0], f.x[j][1]));
+      const Fragment<kWide> xf(f.x[j][0], f.x[j][1]);
       const float s = f.s[j] * f.ws;
 #pragma unroll
-      for (int v = 0; v < 4; ++v) acc[j][v] += block[v] * s;
+      for (int i = 0; i < RT; ++i) {
+        const floatx4 block = multiply(Fragment<kWide>(f.w[i][0], f.w[i][1]), xf);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) acc[i][j][v] += block[v] * s;
+      }
     }
   };
   for (int block = wave; block < a.blocks; block += 2 * kFewWaves) {
@@ -253,14 +263,16 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(ProductArgs
     if (block + kFewWaves < a.blocks) work(f[1]);
   }
 #pragma unroll
-  for (int j = 0; j < MT; ++j) sums[wave][j][lane] = acc[j];
-  __syncthreads();
-  const int r = r0 + fq * 4;
-  for (int j = wave; j < MT; j += kFewWaves) {
-    floatx4 sum = sums[0][j][lane];
+  for (int i = 0; i < RT; ++i)
 #pragma unroll
-    for (int w = 1; w < kFewWaves; ++w) sum += sums[w][j][lane];
-    const int64_t m = m0 + j * 16 + fr;
+    for (int j = 0; j < MT; ++j) sums[wave][i * MT + j][lane] = acc[i][j];
+  __syncthreads();
+  for (int tile = wave; tile < RT * MT; tile += kFewWaves) {
+    floatx4 sum = sums[0][tile][lane];
+#pragma unroll
+    for (int w = 1; w < kFewWaves; ++w) sum += sums[w][tile][lane];
+    const int r = r0 + tile / MT * 16 + fq * 4;
+    const int64_t m = m0 + tile % MT * 16 + fr;
     if (m >= a.vectors || r >= a.rows) continue;
     store_four(out + row_offset(m, a.batch, a.out_step, a.out_sample, a.out_even), r, a.rows, sum + bias_of(a.bias, r, a.rows));
   }
@@ -456,8 +468,8 @@ hipError_t run_product(ProductArgs a, const sprnn_seq_t& out, hipStream_t stream
   // Few rows, or outputs of fewer 128 x 128 tiles than half of the CUs.
   if (a.vectors <= 64 || groups(kTileM, kTileR) < 128) {
     const int rows = a.vectors <= 16 ? 16 : a.vectors <= 32 ? 32 : 64;
-    auto kernel = rows == 16 ? product_few_kernel<TYPE, 1> : rows == 32 ? product_few_kernel<TYPE, 2> : product_few_kernel<TYPE, 4>;
-    return launch(kernel, dim3((unsigned)groups(rows, 16)), dim3(64 * kFewWaves), 0, stream, a, to);
+    auto kernel = rows == 16 ? product_few_kernel<TYPE, 1, 1> : rows == 32 ? product_few_kernel<TYPE, 2, 2> : product_few_kernel<TYPE, 4, 2>;
+    return launch(kernel, dim3((unsigned)groups(rows, rows == 16 ? 16 : 32)), dim3(64 * kFewWaves), 0, stream, a, to);
   }
   // Copies of 16 bytes need rows that begin and end at multiples of them.
   if (a.inputs % 16 == 0 && aligned_to(a.x, 16) && aligned_to(a.w, 16) && a.x_step % 16 == 0 && a.x_sample % 16 == 0) {
