@@ -50,6 +50,14 @@ __device__ __forceinline__ uint4 load_piece(const uint8_t* row, int k, int input
   return v;
 }
 
+__device__ __attribute__((aligned(16))) const uint8_t nothing[16] = {};   // what whole pieces behind a row's end are read from
+// The same for rows that are whole pieces long: no branch around a load in flight.
+__device__ __forceinline__ uint4 load_whole_piece(const uint8_t* row, int k, int inputs) {
+  uint4 v;
+  __builtin_memcpy(&v, k < inputs ? row + k : nothing, 16);
+  return v;
+}
+
 // Rows of 128 bytes repeat their banks every other row: piece q (16 bytes) of a row changes places with the row's upper
 // bits, so that the sixteen rows that an LDS cycle serves are in sixteen different groups of banks.
 __device__ __forceinline__ int piece_at(int row, int q) { return row * kSlab + ((q ^ ((row >> 1) & 7)) << 4); }
@@ -198,7 +206,7 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, Elemen
 // the eight sums meet in LDS.  (8 x 2304 x 9216 on 128 x 128 tiles: 28 us, 72 workgroups; here 9.  RT = 2 halves how often
 // many rows of x are fetched.)
 constexpr int kFewWaves = 8;
-template <int TYPE, int MT, int RT>
+template <int TYPE, int MT, int RT, bool WHOLE>
 __global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(ProductArgs a, Element<TYPE>* out) {
   constexpr bool kWide = TYPE == SPRNN_TYPE_F32;
   __shared__ floatx4 sums[kFewWaves][RT * MT][64];
@@ -223,17 +231,18 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(ProductArgs
     uint4 w[RT][2], x[MT][2];
     float s[MT], ws;
   };
+  auto load = [&](const uint8_t* row, int k) { return WHOLE ? load_whole_piece(row, k, a.inputs) : load_piece(row, k, a.inputs); };
   auto fetch = [&](Block& f, int block) {
     const int at = min(block, a.blocks - 1), k = at * kSlab + fq * 16;
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) f.w[i][h] = load_piece(w_row[i], k + 64 * h, a.inputs);
+      for (int h = 0; h < 2; ++h) f.w[i][h] = load(w_row[i], k + 64 * h);
     f.ws = w_scale[at];
 #pragma unroll
     for (int j = 0; j < MT; ++j) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) f.x[j][h] = load_piece(x_row[j], k + 64 * h, a.inputs);
+      for (int h = 0; h < 2; ++h) f.x[j][h] = load(x_row[j], k + 64 * h);
       f.s[j] = scale_row[j][at];
     }
   };
@@ -295,7 +304,6 @@ template <int IR> constexpr int many_r() { return Many<IR>::kWR * IR * 32; }
 template <int IR> constexpr int many_m() { return Many<IR>::kWM * 64; }
 template <int IR> constexpr int many_threads() { return Many<IR>::kWR * Many<IR>::kWM * 64; }
 template <int IR> constexpr int many_stage() { return (many_r<IR>() + many_m<IR>()) * kSlab; }
-__device__ __attribute__((aligned(16))) const uint8_t nothing[16] = {};   // what pieces behind a row's end are copied from
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 // 32 rows of a slab: this lane's four pieces, every other one of its row.
@@ -468,7 +476,12 @@ hipError_t run_product(ProductArgs a, const sprnn_seq_t& out, hipStream_t stream
   // Few rows, or outputs of fewer 128 x 128 tiles than half of the CUs.
   if (a.vectors <= 64 || groups(kTileM, kTileR) < 128) {
     const int rows = a.vectors <= 16 ? 16 : a.vectors <= 32 ? 32 : 64;
-    auto kernel = rows == 16 ? product_few_kernel<TYPE, 1, 1> : rows == 32 ? product_few_kernel<TYPE, 2, 2> : product_few_kernel<TYPE, 4, 2>;
+    auto kernel = a.inputs % 16 == 0 ? rows == 16   ? product_few_kernel<TYPE, 1, 1, true>
+                                       : rows == 32 ? product_few_kernel<TYPE, 2, 2, true>
+                                                    : product_few_kernel<TYPE, 4, 2, true>
+                  : rows == 16       ? product_few_kernel<TYPE, 1, 1, false>
+                  : rows == 32       ? product_few_kernel<TYPE, 2, 2, false>
+                                     : product_few_kernel<TYPE, 4, 2, false>;
     return launch(kernel, dim3((unsigned)groups(rows, rows == 16 ? 16 : 32)), dim3(64 * kFewWaves), 0, stream, a, to);
   }
   // Copies of 16 bytes need rows that begin and end at multiples of them.
