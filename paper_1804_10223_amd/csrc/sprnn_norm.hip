@@ -8,7 +8,7 @@
 // row at a time, eight consecutive elements a lane and pass, with as many wavefronts as one pass needs (rows of up to 8192;
 // wider ones take two passes), so that no lane is idle in any but the last wavefront and a block of 128 elements is
 // a DPP row of 16 lanes.  It fetches its next row before it sums the present one.  Rows wider than 16384 are read twice.
-#include "sprnn_seq.h"
+#include "sprnn_sums.h"
 
 namespace sprnn {
 namespace {
@@ -324,29 +324,10 @@ __global__ __launch_bounds__(1024) void norm_backward_wide_kernel(NormArgs a, Vi
   }
 }
 
-// out[i] = sum of partial[j][i] over j < count: 64 columns a workgroup, whose 16 wavefronts share out j.
-__global__ __launch_bounds__(1024) void sum_partials_kernel(const float* partial, int count, int64_t width, float* out) {
-  __shared__ float sums[16][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t i = (int64_t)blockIdx.x * 64 + lane;
-  float sum = 0.0f;
-  if (i < width) {
-    int j = wave;
-    for (; j + 48 < count; j += 64) {
-      const float p0 = partial[(int64_t)j * width + i], p1 = partial[(int64_t)(j + 16) * width + i];
-      const float p2 = partial[(int64_t)(j + 32) * width + i], p3 = partial[(int64_t)(j + 48) * width + i];
-      sum += (p0 + p1) + (p2 + p3);
-    }
-    for (; j < count; j += 16) sum += partial[(int64_t)j * width + i];
-  }
-  sums[wave][lane] = sum;
-  __syncthreads();
-  if (wave == 0 && i < width) {
-#pragma unroll
-    for (int w = 1; w < 16; ++w) sum += sums[w][lane];
-    out[i] = sum;
-  }
-}
+struct PutWeight {
+  float* out;
+  __device__ void operator()(int64_t i, float sum) const { out[i] = sum; }
+};
 
 struct Shape {
   int waves, passes;   // passes 0: the row does not fit in registers
@@ -393,8 +374,7 @@ hipError_t run_backward(const NormArgs& a, const sprnn_seq_t& dy, const sprnn_se
     if (e != hipSuccess) return e;
   }
   if (!d_weight) return hipSuccess;
-  return launch(sum_partials_kernel, dim3((unsigned)((a.width + 63) / 64)), dim3(1024), 0, stream, (const float*)partial, groups,
-                (int64_t)a.width, d_weight);
+  return launch_sum_partials(partial, groups, (int64_t)a.width, PutWeight{d_weight}, stream);
 }
 
 bool good_norm(const sprnn_norm_t* n) {
@@ -406,10 +386,6 @@ NormArgs arguments(const sprnn_norm_t* n, float* scales) {
 }
 
 }  // namespace
-
-hipError_t launch_sum_partials(const float* partial, int count, int64_t width, float* out, hipStream_t stream) {
-  return launch(sum_partials_kernel, dim3((unsigned)((width + 63) / 64)), dim3(1024), 0, stream, partial, count, width, out);
-}
 
 }  // namespace sprnn
 

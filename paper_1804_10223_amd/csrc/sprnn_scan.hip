@@ -429,7 +429,8 @@ int sprnn_scan_backward(int device_id, const sprnn_scan_t* scan, sprnn_seq_t dy,
       return SPRNN_ERR_INVALID;
     if (g.z.data && !scan->z.data) return SPRNN_ERR_INVALID;
   }
-  if (!workspace || !aligned_to(workspace, 16) || workspace_bytes < scan_backward_bytes(s)) return SPRNN_ERR_INVALID;
+  const int64_t need = scan_backward_bytes(s);
+  if (need > 0 && (!workspace || !aligned_to(workspace, 16) || workspace_bytes < need)) return SPRNN_ERR_INVALID;
   DeviceGuard guard(device_id);
   if (!guard.ok) return SPRNN_ERR_HIP;
   return SPRNN_HIP(launch_scan_backward(s, scan, dy, d_state_out, static_cast<const float*>(kept), gradients, static_cast<float*>(workspace),

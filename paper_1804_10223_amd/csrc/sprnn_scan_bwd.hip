@@ -15,11 +15,9 @@
 // a workgroup meet in LDS.  Everything that depends on (step, channel) alone is done once, with one lane a channel, before
 // and after the states' work, and handed over through LDS.
 #include "sprnn_scan.h"
+#include "sprnn_sums.h"
 
 namespace sprnn {
-
-hipError_t launch_sum_partials(const float* partial, int count, int64_t width, float* out, hipStream_t stream);
-
 namespace {
 
 // A segment's effect on the adjoint, from zero behind it: like the forward pass's, from the end.
@@ -404,16 +402,24 @@ __global__ __launch_bounds__(256) void scan_low_gradients_kernel(ScanArgs a, int
   out.row(t, b)[(int64_t)group * a.N + n] = (Element<TYPE>)sum;
 }
 
-// dA, dD and d dt_bias from their sums [quads * C * 4, C, C].
-__global__ __launch_bounds__(256) void scan_parameter_gradients_kernel(int C, int N, int quads, const float* sums, float* dA, float* dD, float* dbias) {
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (at >= (int64_t)C * N) return;
-  const int c = (int)(at / N), n = (int)(at % N);
-  const int64_t states = (int64_t)quads * C * 4;
-  if (dA) dA[at] = sums[((int64_t)(n >> 2) * C + c) * 4 + (n & 3)];
-  if (n == 0 && dD) dD[c] = sums[states + c];
-  if (n == 0 && dbias) dbias[c] = sums[states + C + c];
-}
+// Sums [quads][C][4], [C], [C] to dA [C][N], dD and d dt_bias [C].
+struct PutParameters {
+  float* dA;
+  float* dD;
+  float* dbias;
+  int C, N;
+  int64_t states;                      // quads * C * 4
+  __device__ void operator()(int64_t i, float sum) const {
+    if (i < states) {
+      const int c = (int)(i / 4 % C), n = (int)(i / 4 / C) * 4 + (int)(i & 3);
+      if (dA && n < N) dA[(int64_t)c * N + n] = sum;
+    } else if (i < states + C) {
+      if (dD) dD[i - states] = sum;
+    } else if (dbias) {
+      dbias[i - states - C] = sum;
+    }
+  }
+};
 
 int lanes_of(int quads) {
   int S = 1;
@@ -426,7 +432,7 @@ int blocks_of(const ScanShape& s, int S) {
 }
 
 struct Workspace {   // in floats
-  int64_t carry, sums, partial, totals, reduced, all;
+  int64_t carry, sums, partial, totals, all;
 };
 Workspace layout(const ScanShape& s) {
   const int S = lanes_of(s.quads);
@@ -438,7 +444,6 @@ Workspace layout(const ScanShape& s) {
   w.sums = take(s.back_segments > 1 ? (int64_t)s.back_segments * s.B * s.C : 0);
   w.partial = take((int64_t)blocks_of(s, S) * s.T * s.B * s.G * 8 * S);
   w.totals = take(s.back_segments * s.B * width);
-  w.reduced = take(width);
   w.all = at;
   return w;
 }
@@ -477,10 +482,8 @@ hipError_t run(const ScanShape& s, const sprnn_scan_t* p, const sprnn_seq_t& dy,
     }
   }
   if (!out->A && !out->D && !out->dt_bias) return hipSuccess;
-  e = launch_sum_partials(workspace + w.totals, s.back_segments * s.B, width, workspace + w.reduced, stream);
-  if (e != hipSuccess) return e;
-  return launch(scan_parameter_gradients_kernel, dim3((unsigned)(((int64_t)s.C * s.N + 255) / 256)), dim3(256), 0, stream, s.C, s.N, s.quads,
-                (const float*)(workspace + w.reduced), out->A, out->D, out->dt_bias);
+  return launch_sum_partials(workspace + w.totals, s.back_segments * s.B, width,
+                             PutParameters{out->A, out->D, out->dt_bias, s.C, s.N, (int64_t)s.quads * s.C * 4}, stream);
 }
 
 template <int TYPE>
