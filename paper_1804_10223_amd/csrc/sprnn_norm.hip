@@ -7,7 +7,11 @@
 // Bound by bytes: a row is read once, kept in registers while its sum is formed, and written once.  A workgroup takes one
 // row at a time, eight consecutive elements a lane and pass, with as many wavefronts as one pass needs (rows of up to 8192;
 // wider ones take two passes), so that no lane is idle in any but the last wavefront and a block of 128 elements is
-// a DPP row of 16 lanes.  It fetches its next row before it sums the present one.  Rows wider than 16384 are read twice.
+// a DPP row of 16 lanes.  It loads its next row before it sums the present one; 16 wavefronts a compute unit then keep enough
+// bytes in flight, and later workgroups would only begin with nothing in flight.  Rows wider than 16384, and two-pass rows that
+// are not whole (below), are read twice.  Measured, bfloat16 with a float32 residual stream: 8192 x 2304 to e4m3 35 us
+// (5.9 TB/s; 108 -> 82 us where nothing is in a cache when the loads waited in front of the sums), backward 4096 x 2560
+// 30 us (4.9 TB/s).
 #include "sprnn_sums.h"
 
 namespace sprnn {
@@ -35,10 +39,33 @@ __device__ __forceinline__ Pack<E, kV> load_row(const E* row, int at, int width)
   if (at + kV <= width) return load_pack<kV>(row + at);
   return load_part<kV>(row + at, width - at);
 }
-template <typename E>
+template <bool WHOLE = false, typename E>
 __device__ __forceinline__ void store_row(E* row, int at, int width, const Pack<E, kV>& p) {
-  if (at + kV <= width) store_pack(row + at, p);
+  if (WHOLE || at + kV <= width) store_pack(row + at, p);
   else store_part(row + at, p, width - at);
+}
+
+// Eight elements of the row at `row`, zeros behind its end and of a row that is not there (`there`; a tensor that is not there
+// has no address).  WHOLE: rows are 16-byte aligned and a multiple of eight elements long; they are read through a buffer, whose
+// own check of the range takes the branches' place.  A branch around a load ends with a wait for it: with branches nothing is
+// in flight while a row is worked on.
+template <bool WHOLE, typename E>
+__device__ __forceinline__ Pack<E, kV> fetch_row(const E* row, int at, int width, bool there) {
+  if constexpr (WHOLE) {
+    const uint64_t base = reinterpret_cast<uint64_t>(row);
+    const uint64_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)base), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(base >> 32));
+    const auto buffer = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(lo | hi << 32), 0, there ? width * (int)sizeof(E) : 0, 0x00020000);
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    words v[sizeof(E) / 2];
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(E) / 2; ++i) v[i] = __builtin_amdgcn_raw_buffer_load_b128(buffer, at * (int)sizeof(E) + 16 * i, 0, 0);
+    Pack<E, kV> p;
+    __builtin_memcpy(&p, v, sizeof(p));
+    return p;
+  } else {
+    if (!there || at >= width) return Pack<E, kV>{};
+    return load_row(row, at, width);
+  }
 }
 
 // Sum over the workgroup; `slots` alternates between calls, so that one barrier a call is enough.
@@ -53,8 +80,42 @@ __device__ __forceinline__ float sum_workgroup(float v, float* slots) {
   return total;
 }
 
+// ... of two numbers.
+__device__ __forceinline__ float2 sum_workgroup(float2 v, float2* slots) {
+  const int waves = blockDim.x >> 6;
+  v.x = sum_lanes<64>(v.x);
+  v.y = sum_lanes<64>(v.y);
+  if (waves == 1) return v;
+  if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float2 total = slots[0];
+  for (int w = 1; w < waves; ++w) { total.x += slots[w].x; total.y += slots[w].y; }
+  return total;
+}
+
+// A lane's weights; 1 without any.
+__device__ __forceinline__ void load_weight(const float* weight, int at, int width, float (&w)[kV]) {
+#pragma unroll
+  for (int i = 0; i < kV; ++i) w[i] = 1.0f;
+  if (weight && at < width) widen(load_row(weight, at, width), w);
+}
+
+// The rows of a workgroup: every gridDim.x-th, found without a division after the first.
+struct RowCursor {
+  uint32_t row, rows, batch, t, b, by_t, by_b;
+  __device__ __forceinline__ RowCursor(uint32_t rows, uint32_t batch)
+      : row(blockIdx.x), rows(rows), batch(batch), t(row / batch), b(row - t * batch), by_t(gridDim.x / batch), by_b(gridDim.x - by_t * batch) {}
+  __device__ __forceinline__ bool there() const { return row < rows; }
+  __device__ __forceinline__ void forth() {
+    row += gridDim.x;
+    t += by_t;
+    b += by_b;
+    if (b >= batch) { b -= batch; ++t; }
+  }
+};
+
 struct NormArgs {
-  int64_t rows;
+  uint32_t rows;
   int batch, width;
   float eps, inv_width;
   const float* weight;
@@ -86,7 +147,7 @@ __device__ __forceinline__ void store_e4m3(const float (&y)[kV], uint8_t* row, i
   if ((threadIdx.x & 15) == 0) scale_at[at >> 7] = scale;
 }
 
-template <int TYPE, int RTYPE, int P, bool E4M3>
+template <int TYPE, int RTYPE, int P, bool E4M3, bool WHOLE>
 __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a, View<const Element<TYPE>> x, View<const Element<RTYPE>> res,
                                                     View<Element<RTYPE>> res_out, View<uint8_t> y8, View<Element<TYPE>> y) {
   typedef Element<TYPE> E;
@@ -96,49 +157,39 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a, View<const Eleme
   const int blocks = (a.width + 127) >> 7;
   float w[P][kV];
 #pragma unroll
-  for (int p = 0; p < P; ++p) {
-    const int at = first + p * stride;
-#pragma unroll
-    for (int i = 0; i < kV; ++i) w[p][i] = a.weight && at + i < a.width ? a.weight[at + i] : 1.0f;
-  }
-  Pack<E, kV> xs[P];
-  Pack<R, kV> rs[P];
-  auto fetch = [&](int64_t row) {
-    const int64_t t = row / a.batch, b = row - t * a.batch;
+  for (int p = 0; p < P; ++p) load_weight(a.weight, first + p * stride, a.width, w[p]);
+  struct Fetched {
+    Pack<E, kV> x[P];
+    Pack<R, kV> res[P];
+  };
+  auto fetch = [&](Fetched& to, const RowCursor& from) {
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int at = first + p * stride;
-      if (at < a.width) {
-        xs[p] = load_row(x.row(t, b), at, a.width);
-        if (res.data) rs[p] = load_row(res.row(t, b), at, a.width);
-      }
+      to.x[p] = fetch_row<WHOLE>(x.row(from.t, from.b), at, a.width, from.there());
+      to.res[p] = fetch_row<WHOLE>(res.row(from.t, from.b), at, a.width, from.there() && res.data);
     }
   };
-  int64_t row = blockIdx.x;
-  if (row < a.rows) fetch(row);
-  for (int turn = 0; row < a.rows; row += gridDim.x, turn ^= 1) {
-    const int64_t t = row / a.batch, b = row - t * a.batch;
+  RowCursor now(a.rows, a.batch);
+  auto work = [&](const Fetched& own, Fetched& next, int turn) {
     float r[P][kV], sum = 0.0f;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int at = first + p * stride;
+      float f[kV];
+      widen(own.x[p], r[p]);
+      widen(own.res[p], f);
 #pragma unroll
-      for (int i = 0; i < kV; ++i) r[p][i] = 0.0f;
-      if (at >= a.width) continue;
-      widen(xs[p], r[p]);
-      if (res.data) {
-        float f[kV];
-        widen(rs[p], f);
-#pragma unroll
-        for (int i = 0; i < kV; ++i) r[p][i] += f[i];
-      }
+      for (int i = 0; i < kV; ++i) r[p][i] += f[i];
       const Pack<R, kV> kept = narrow<R>(r[p]);      // the stream that goes on is what is normed
-      if (res_out.data) store_row(res_out.row(t, b), at, a.width, kept);
-      if (RTYPE != SPRNN_TYPE_F32 && res.data) widen(kept, r[p]);
+      if (res_out.data && at < a.width) store_row<WHOLE>(res_out.row(now.t, now.b), at, a.width, kept);
+      if (RTYPE != SPRNN_TYPE_F32) widen(kept, r[p]);
 #pragma unroll
       for (int i = 0; i < kV; ++i) sum += r[p][i] * r[p][i];
     }
-    if (row + gridDim.x < a.rows) fetch(row + gridDim.x);
+    RowCursor ahead = now;
+    ahead.forth();
+    fetch(next, ahead);
     const float scale = 1.0f / sqrtf(sum_workgroup(sum, slots[turn]) * a.inv_width + a.eps);
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -146,9 +197,17 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a, View<const Eleme
       if (!E4M3 && at >= a.width) continue;
 #pragma unroll
       for (int i = 0; i < kV; ++i) r[p][i] = r[p][i] * scale * w[p][i];
-      if (E4M3) store_e4m3(r[p], y8.row(t, b), at, a.width, a.scales + row * blocks);
-      else store_row(y.row(t, b), at, a.width, narrow<E>(r[p]));
+      if (E4M3) store_e4m3(r[p], y8.row(now.t, now.b), at, a.width, a.scales + (int64_t)now.row * blocks);
+      else store_row<WHOLE>(y.row(now.t, now.b), at, a.width, narrow<E>(r[p]));
     }
+    now = ahead;
+  };
+  Fetched one, two;                                  // in turn: a copy of what is in flight would wait for it
+  fetch(one, now);
+  while (now.there()) {
+    work(one, two, 0);
+    if (!now.there()) break;
+    work(two, one, 1);
   }
 }
 
@@ -204,51 +263,54 @@ __global__ __launch_bounds__(1024) void norm_wide_kernel(NormArgs a, View<const 
 
 // Backward pass of rows that fit a workgroup's registers; the weight's gradient is summed over a workgroup's rows in
 // registers and left in `partial` [workgroup][width].
-template <int TYPE, int RTYPE>
+template <int TYPE, int RTYPE, bool WHOLE>
 __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs a, View<const Element<TYPE>> dy, View<const Element<RTYPE>> r,
                                                              View<const Element<RTYPE>> d_res, View<Element<RTYPE>> dr,
                                                              float* partial) {
   typedef Element<TYPE> E;
   typedef Element<RTYPE> R;
-  __shared__ float slots[2][2][kMaxWaves];
+  __shared__ float2 slots[2][kMaxWaves];
   const int first = threadIdx.x * kV;
-  auto weight = [&](int at, int i) { return a.weight && at + i < a.width ? a.weight[at + i] : 1.0f; };
   float* const mine = partial ? partial + (int64_t)blockIdx.x * a.width : nullptr;
-  float w[kV], dw[kV];
-#pragma unroll
-  for (int i = 0; i < kV; ++i) { w[i] = weight(first, i); dw[i] = 0.0f; }
-  Pack<R, kV> rs_, ds;
-  Pack<E, kV> gs;
-  auto fetch = [&](int64_t row) {
-    const int64_t t = row / a.batch, b = row - t * a.batch;
-    if (first < a.width) {
-      rs_ = load_row(r.row(t, b), first, a.width);
-      gs = load_row(dy.row(t, b), first, a.width);
-      if (d_res.data) ds = load_row(d_res.row(t, b), first, a.width);
-    }
+  float w[kV], dw[kV] = {};
+  load_weight(a.weight, first, a.width, w);
+  struct Fetched {
+    Pack<R, kV> r, d;
+    Pack<E, kV> g;
   };
-  int64_t row = blockIdx.x;
-  if (row < a.rows) fetch(row);
-  for (int turn = 0; row < a.rows; row += gridDim.x, turn ^= 1) {
-    const int64_t t = row / a.batch, b = row - t * a.batch;
-    float f[kV] = {}, g[kV] = {}, o[kV] = {}, square = 0.0f, dot = 0.0f;
-    if (first < a.width) {
-      widen(rs_, f);
-      widen(gs, g);
-      if (d_res.data) widen(ds, o);
+  auto fetch = [&](Fetched& to, const RowCursor& from) {
+    to.r = fetch_row<WHOLE>(r.row(from.t, from.b), first, a.width, from.there());
+    to.g = fetch_row<WHOLE>(dy.row(from.t, from.b), first, a.width, from.there());
+    to.d = fetch_row<WHOLE>(d_res.row(from.t, from.b), first, a.width, from.there() && d_res.data);
+  };
+  RowCursor now(a.rows, a.batch);
+  auto work = [&](const Fetched& own, Fetched& next, int turn) {
+    float f[kV], g[kV], o[kV], square = 0.0f, dot = 0.0f;
+    widen(own.r, f);
+    widen(own.g, g);
 #pragma unroll
-      for (int i = 0; i < kV; ++i) { square += f[i] * f[i]; dot += f[i] * (g[i] * w[i]); }
-    }
-    if (row + gridDim.x < a.rows) fetch(row + gridDim.x);
-    const float rs = 1.0f / sqrtf(sum_workgroup(square, slots[turn][0]) * a.inv_width + a.eps);
-    const float along = sum_workgroup(dot, slots[turn][1]) * a.inv_width * rs * rs;   // mean(dy w n) rs: n = f rs takes one more
-    if (first >= a.width) continue;
+    for (int i = 0; i < kV; ++i) { square += f[i] * f[i]; dot += f[i] * (g[i] * w[i]); }
+    RowCursor ahead = now;
+    ahead.forth();
+    fetch(next, ahead);
+    const float2 sums = sum_workgroup(make_float2(square, dot), slots[turn]);
+    const float rs = 1.0f / sqrtf(sums.x * a.inv_width + a.eps);
+    const float along = sums.y * a.inv_width * rs * rs;   // mean(dy w n) rs: n = f rs takes one more
+    widen(own.d, o);
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
       dw[i] += g[i] * (f[i] * rs);
       o[i] += rs * (g[i] * w[i] - f[i] * along);
     }
-    store_row(dr.row(t, b), first, a.width, narrow<R>(o));
+    if (first < a.width) store_row<WHOLE>(dr.row(now.t, now.b), first, a.width, narrow<R>(o));
+    now = ahead;
+  };
+  Fetched one, two;                                  // in turn: a copy of what is in flight would wait for it
+  fetch(one, now);
+  while (now.there()) {
+    work(one, two, 0);
+    if (!now.there()) break;
+    work(two, one, 1);
   }
   if (mine && first < a.width) {
     Pack<float, kV> out;
@@ -265,7 +327,7 @@ __global__ __launch_bounds__(1024) void norm_backward_wide_kernel(NormArgs a, Vi
                                                                   View<const Element<RTYPE>> r, View<const Element<RTYPE>> d_res,
                                                                   View<Element<RTYPE>> dr, float* partial) {
   typedef Element<RTYPE> R;
-  __shared__ float slots[2][2][kMaxWaves];
+  __shared__ float2 slots[2][kMaxWaves];
   const int first = threadIdx.x * kV, stride = blockDim.x * kV;
   auto weight = [&](int at, int i) { return a.weight && at + i < a.width ? a.weight[at + i] : 1.0f; };
   float* const mine = partial ? partial + (int64_t)blockIdx.x * a.width : nullptr;
@@ -291,8 +353,9 @@ __global__ __launch_bounds__(1024) void norm_backward_wide_kernel(NormArgs a, Vi
 #pragma unroll kKept
     for (int p = 0; p < passes; ++p)
       if (first + p * stride < a.width) sum(first + p * stride);
-    const float rs = 1.0f / sqrtf(sum_workgroup(square, slots[turn][0]) * a.inv_width + a.eps);
-    const float along = sum_workgroup(dot, slots[turn][1]) * a.inv_width * rs * rs;
+    const float2 sums = sum_workgroup(make_float2(square, dot), slots[turn]);
+    const float rs = 1.0f / sqrtf(sums.x * a.inv_width + a.eps);
+    const float along = sums.y * a.inv_width * rs * rs;
     auto finish = [&](int at, float (&d)[kV], bool in_memory) {
       float f[kV], g[kV], o[kV] = {};
       widen(load_row(r.row(t, b), at, a.width), f);
@@ -340,11 +403,16 @@ Shape shape_of(int width) {
   }
   return {kMaxWaves, 0};
 }
-// Workgroups of the backward pass: enough wavefronts to keep the memory busy, few enough that the partial sums are small
-// beside the rows.
+// Every row of the view is 16-byte aligned and a whole number of lanes' elements.
+bool whole_rows(const sprnn_seq_t& s, int type, int width) {
+  const int64_t per_16 = 16 / type_bytes(type);
+  return width % kV == 0 && aligned_to(s.data, 16) && s.step % per_16 == 0 && s.sample % per_16 == 0;
+}
+// Workgroups of the backward pass: ten wavefronts a compute unit keep the memory busy; more only leave more partial sums
+// of the weight's gradient (4096 x 2560 as above, 16 wavefronts 35.5 us, 10 30.0; 16384 x 1024 53 and 50).
 int backward_groups(int64_t rows, int width) {
   const int waves = shape_of(width).waves;
-  const int64_t most = waves <= 2 ? 2048 : waves <= 4 ? 1024 : 512;
+  const int64_t most = (int64_t)256 * (waves < 10 ? 10 / waves : 1);
   return (int)(rows < most ? rows : most);
 }
 
@@ -352,10 +420,11 @@ template <int TYPE, int RTYPE, bool E4M3>
 hipError_t run_norm(const NormArgs& a, const sprnn_seq_t& x, const sprnn_seq_t& res, const sprnn_seq_t& res_out,
                     const sprnn_seq_t& y, hipStream_t stream) {
   const Shape s = shape_of(a.width);
-  const int64_t most = (int64_t)256 * (s.waves <= 2 ? 16 : s.waves <= 8 ? 6 : 2);
-  const dim3 grid((unsigned)(a.rows < most ? a.rows : most)), block((unsigned)s.waves * 64);
-  auto kernel = s.passes == 1 ? norm_kernel<TYPE, RTYPE, 1, E4M3> : s.passes == 2 ? norm_kernel<TYPE, RTYPE, 2, E4M3>
-              : norm_wide_kernel<TYPE, RTYPE, E4M3>;
+  const int64_t most = (int64_t)256 * (s.waves < 16 ? 16 / s.waves : 1);
+  const dim3 grid((unsigned)((int64_t)a.rows < most ? a.rows : most)), block((unsigned)s.waves * 64);
+  const bool whole = whole_rows(x, TYPE, a.width) && (!res.data || whole_rows(res, RTYPE, a.width));
+  auto kernel = s.passes == 1 ? whole ? norm_kernel<TYPE, RTYPE, 1, E4M3, true> : norm_kernel<TYPE, RTYPE, 1, E4M3, false>
+              : s.passes == 2 && whole ? norm_kernel<TYPE, RTYPE, 2, E4M3, true> : norm_wide_kernel<TYPE, RTYPE, E4M3>;
   return launch(kernel, grid, block, 0, stream, a, view<const Element<TYPE>>(x), view<const Element<RTYPE>>(res),
                 view<Element<RTYPE>>(res_out), view<uint8_t>(y), view<Element<TYPE>>(y));
 }
@@ -364,9 +433,11 @@ template <int TYPE, int RTYPE>
 hipError_t run_backward(const NormArgs& a, const sprnn_seq_t& dy, const sprnn_seq_t& r, const sprnn_seq_t& d_res,
                         const sprnn_seq_t& dr, float* d_weight, float* partial, hipStream_t stream) {
   const Shape s = shape_of(a.width);
-  const int groups = backward_groups(a.rows, a.width);
+  const int groups = backward_groups((int64_t)a.rows, a.width);
   if (groups > 0) {
-    auto kernel = s.passes == 1 ? norm_backward_kernel<TYPE, RTYPE> : s.passes == 2 ? norm_backward_wide_kernel<TYPE, RTYPE, 2>
+    const bool whole = whole_rows(dy, TYPE, a.width) && whole_rows(r, RTYPE, a.width) && (!d_res.data || whole_rows(d_res, RTYPE, a.width));
+    auto kernel = s.passes == 1 ? whole ? norm_backward_kernel<TYPE, RTYPE, true> : norm_backward_kernel<TYPE, RTYPE, false>
+                                : s.passes == 2 ? norm_backward_wide_kernel<TYPE, RTYPE, 2>
                                 : norm_backward_wide_kernel<TYPE, RTYPE, 0>;
     const hipError_t e = launch(kernel, dim3((unsigned)groups), dim3((unsigned)s.waves * 64), 0, stream, a, view<const Element<TYPE>>(dy),
                                 view<const Element<RTYPE>>(r), view<const Element<RTYPE>>(d_res), view<Element<RTYPE>>(dr),
@@ -382,7 +453,7 @@ bool good_norm(const sprnn_norm_t* n) {
          (n->residual_type == n->type || n->residual_type == SPRNN_TYPE_F32) && n->eps >= 0.0f && aligned_to(n->weight, 4);
 }
 NormArgs arguments(const sprnn_norm_t* n, float* scales) {
-  return NormArgs{(int64_t)n->steps * n->batch, n->batch, n->width, n->eps, 1.0f / (float)n->width, n->weight, scales};
+  return NormArgs{(uint32_t)((int64_t)n->steps * n->batch), n->batch, n->width, n->eps, 1.0f / (float)n->width, n->weight, scales};
 }
 
 }  // namespace
