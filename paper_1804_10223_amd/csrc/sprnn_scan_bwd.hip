@@ -171,7 +171,8 @@ __global__ __launch_bounds__(64 * waves_of(S), 2) void scan_backward_kernel(Scan
   typedef Element<TYPE> E;
   constexpr int W = waves_of(S), R = lane_channels(S), CW = wave_channels(S), CL = 64 / S;
   constexpr int kItems = kTile * CW / 64;      // (step, channel) pairs of a lane
-  constexpr int kRow = 4 * S, kOwn = kTile * 2 * kRow / 64;
+  constexpr int kRow = 4 * S;
+  constexpr bool kStartAhead = S < 32;         // a channel's first states are loaded a channel ahead; at S = 32 they are three registers too many
   // [d, later sum g B][d u, later sum through A][e, later y] of every (step, channel); B and C of the tile; sums over channels
   __shared__ float hand[W][3][kTile][CW];
   __shared__ __attribute__((aligned(16))) float low[2][kTile][2][kRow];
@@ -208,39 +209,61 @@ __global__ __launch_bounds__(64 * waves_of(S), 2) void scan_backward_kernel(Scan
   Cursor<E> du_at(io.du, last, b), ddt_at(io.ddt, last, b), dz_at(io.dz, last, b);
   Cursor<const E> B_at(io.B, last, b, group * a.N), C_at(io.C, last, b, group * a.N);
   const bool gated = io.z.data != nullptr;
+  // Items and rows of B and C are loaded a tile ahead, behind the states' work (whose registers they take), and this tile's
+  // items again at the same place: their latency passes under the sums.  No load stands under a branch: it would be waited for.
+  struct Items {
+    E u[kItems], dt[kItems], z[kItems], dy[kItems];
+  };
+  auto fetch_items = [&](Items& to, int rows) {
+    load_items<CW>(to.u, u_at.template tile<true>(rows, a.C), lane, c_item);
+    load_items<CW>(to.dt, dt_at.template tile<true>(rows, a.C), lane, c_item);
+    load_items<CW>(to.z, z_at.template tile<true>(rows, gated ? a.C : 0), lane, c_item);
+    load_items<CW>(to.dy, dy_at.template tile<true>(rows, a.C), lane, c_item);
+  };
+  constexpr int kLow = (kTile * kRow + 64 * W - 1) / (64 * W);
+  E B_next[kLow], C_next[kLow];
+  auto low_item = [&](int i) { return min((int)threadIdx.x + i * 64 * W, kTile * kRow - 1); };   // (several lanes may have the last)
+  auto fetch_low = [&](int rows) {
+    const Tile<const E> B_rows = B_at.template tile<true>(rows, a.N), C_rows = C_at.template tile<true>(rows, a.N);
+    B_at.back(); C_at.back();
+#pragma unroll
+    for (int i = 0; i < kLow; ++i) {
+      B_next[i] = B_rows.load(low_item(i) / kRow, low_item(i) % kRow);
+      C_next[i] = C_rows.load(low_item(i) / kRow, low_item(i) % kRow);
+    }
+  };
+  Items next;
+  fetch_items(next, live - last);
+  fetch_low(live - last);
   int buffer = 0;
   for (int t = last; t >= t0 && live > t0; t -= kTile, buffer ^= 1) {
     // what depends on (step, channel) alone
     {
-      const Tile<const E> u_rows = u_at.template tile<true>(live - t, a.C), dt_rows = dt_at.template tile<true>(live - t, a.C), z_rows = z_at.template tile<true>(live - t, gated ? a.C : 0), dy_rows = dy_at.template tile<true>(live - t, a.C);
-      E u[kItems], dt[kItems], z[kItems], dy[kItems];
-      load_items<CW>(u, u_rows, lane, c_item);
-      load_items<CW>(dt, dt_rows, lane, c_item);
-      load_items<CW>(z, z_rows, lane, c_item);
-      load_items<CW>(dy, dy_rows, lane, c_item);
-      const Tile<const E> B_rows = B_at.template tile<true>(live - t, a.N), C_rows = C_at.template tile<true>(live - t, a.N);
-      B_at.back(); C_at.back();
-      for (int i = threadIdx.x; i < kTile * kRow; i += 64 * W) {
-        const int n = i % kRow, q = i / kRow;
-        const bool in = n < a.N && t + q < live;
-        const float Bv = (float)B_rows.load(q, n), Cv = (float)C_rows.load(q, n);
-        low[buffer][q][0][n] = in ? Bv : 0.0f;
-        low[buffer][q][1][n] = in ? Cv : 0.0f;
-      }
       int rows = live - t;                                   // (asked anew for every item: eight kept answers are 16 scalar registers)
 #pragma unroll
       for (int i = 0; i < kItems; ++i) {
         const int q = item_step(i);
         asm volatile("" : "+v"(rows));
         const bool in = q < rows, counts = in && owned(item_channel);   // else a copy of the group's last channel
-        const float v = (float)dt[i] + bias, gate = (float)z[i];
-        const float d = in ? a.softplus ? softplus(v) : v : 0.0f;
+        const float v = (float)next.dt[i] + bias, z = (float)next.z[i];
+        float smooth = softplus(v), gate = z * sigmoid(z);
+        asm volatile("" : "+v"(smooth), "+v"(gate));         // selected below, not branched around
+        const float d = in ? a.softplus ? smooth : v : 0.0f;
         hand[wave][0][q][item_channel] = d;
-        hand[wave][1][q][item_channel] = counts ? d * (float)u[i] : 0.0f;
-        hand[wave][2][q][item_channel] = counts ? (float)dy[i] * (gated ? gate * sigmoid(gate) : 1.0f) : 0.0f;
+        hand[wave][1][q][item_channel] = counts ? d * (float)next.u[i] : 0.0f;
+        hand[wave][2][q][item_channel] = counts ? (float)next.dy[i] * (gated ? gate : 1.0f) : 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < kLow; ++i) {
+        const int n = low_item(i) % kRow, q = low_item(i) / kRow;
+        const bool in = n < a.N && t + q < live;
+        low[buffer][q][0][n] = in ? (float)B_next[i] : 0.0f;
+        low[buffer][q][1][n] = in ? (float)C_next[i] : 0.0f;
       }
     }
     const States in_front(kept, t / kTile, b, a.B, a.quads, a.C);
+    floatx4_t starts[2];
+    starts[0] = in_front.load(sub, channel(lane / S));
     __syncthreads();
 
     float acc[kSums];
@@ -249,8 +272,10 @@ __global__ __launch_bounds__(64 * waves_of(S), 2) void scan_backward_kernel(Scan
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       __builtin_amdgcn_sched_barrier(0);                     // channels one after the other: their registers are the same
-      const int own = r * CL + lane / S, c = channel(own);
-      const floatx4_t start = in_front.load(sub, c);
+      const int own = r * CL + lane / S;
+      if (!kStartAhead && r > 0) starts[r % 2] = in_front.load(sub, channel(own));
+      const floatx4_t start = starts[r % 2];
+      if (kStartAhead && r + 1 < R) starts[(r + 1) % 2] = in_front.load(sub, channel(own + CL));
       float h[kTile][4], f[kTile][4];
       // What is in LDS is read again for every channel and direction (through offsets that the compiler knows nothing
       // about): kept in registers for the whole tile it is 80 too many.
@@ -297,10 +322,16 @@ __global__ __launch_bounds__(64 * waves_of(S), 2) void scan_backward_kernel(Scan
         through = sum_lanes<S>(through);
         y = sum_lanes<S>(y);
         hand[wave][0][q][own] = gB;                          // by all S lanes, which hold the same
-        hand[wave][1][q][own] = through * kLn2;
+        hand[wave][1][q][own] = through;
         hand[wave][2][q][own] = y;
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
+    Items own;
+    fetch_items(own, live - t);
+    u_at.back(); dt_at.back(); z_at.back(); dy_at.back();
+    fetch_items(next, t > t0 ? kTile : 0);
+    fetch_low(t > t0 ? kTile : 0);
     __builtin_amdgcn_sched_barrier(0);
     sum_channels<S>(acc, lane);
 #pragma unroll
@@ -320,37 +351,28 @@ __global__ __launch_bounds__(64 * waves_of(S), 2) void scan_backward_kernel(Scan
     const Tile<E> du_rows = du_at.template tile<true>(live - t, io.du.data ? a.C : 0), ddt_rows = ddt_at.template tile<true>(live - t, io.ddt.data ? a.C : 0), dz_rows = dz_at.template tile<true>(live - t, io.dz.data ? a.C : 0);
     du_at.back(); ddt_at.back(); dz_at.back();
     if (owned(item_channel)) {
-      const Tile<const E> u_rows = u_at.template tile<true>(live - t, a.C), dt_rows = dt_at.template tile<true>(live - t, a.C), z_rows = z_at.template tile<true>(live - t, gated ? a.C : 0), dy_rows = dy_at.template tile<true>(live - t, a.C);
-      E us[kItems], dts[kItems], zs[kItems], dys[kItems];
-      load_items<CW>(us, u_rows, lane, c_item);
-      load_items<CW>(dts, dt_rows, lane, c_item);
-      load_items<CW>(zs, z_rows, lane, c_item);
-      load_items<CW>(dys, dy_rows, lane, c_item);
       int rows = live - t;
       uint32_t du_to = du_rows.offset(lane / CW, c_item), ddt_to = ddt_rows.offset(lane / CW, c_item), dz_to = dz_rows.offset(lane / CW, c_item);
 #pragma unroll
       for (int i = 0; i < kItems; ++i, du_to += 64 / CW * du_rows.step, ddt_to += 64 / CW * ddt_rows.step, dz_to += 64 / CW * dz_rows.step) {
         const int q = item_step(i);
         asm volatile("" : "+v"(rows));
-        const float gB = hand[wave][0][q][item_channel], through = hand[wave][1][q][item_channel], sum = hand[wave][2][q][item_channel];
+        const float gB = hand[wave][0][q][item_channel], through = hand[wave][1][q][item_channel] * kLn2, sum = hand[wave][2][q][item_channel];
         const bool in = q < rows;
-        const float u = in ? (float)us[i] : 0.0f, v = (float)dts[i] + bias;
-        const float d = a.softplus ? softplus(v) : v;
-        float e = in ? (float)dys[i] : 0.0f;
-        if (gated) {
-          const float z = (float)zs[i], s = sigmoid(z);
-          dz_rows.store_at(dz_to, e * (sum + D * u) * (s * (1.0f + z * (1.0f - s))));
-          e = in ? e * (z * s) : 0.0f;
-        }
+        const float u = in ? (float)own.u[i] : 0.0f, v = (float)own.dt[i] + bias;
+        float smooth = softplus(v), slope = sigmoid(v);
+        const float z = (float)own.z[i], s = sigmoid(z), dy = in ? (float)own.dy[i] : 0.0f;
+        asm volatile("" : "+v"(smooth), "+v"(slope));        // selected, not branched around
+        const float d = a.softplus ? smooth : v;
+        dz_rows.store_at(dz_to, dy * (sum + D * u) * (s * (1.0f + z * (1.0f - s))));
+        const float e = !gated ? dy : in ? dy * (z * s) : 0.0f;
         du_rows.store_at(du_to, d * gB + D * e);
-        float dv = u * gB + through;
-        if (a.softplus && v <= 20.0f) dv *= sigmoid(v);
+        const float dv = (u * gB + through) * (a.softplus ? slope : 1.0f);
         ddt_rows.store_at(ddt_to, dv);
         dD += e * u;
         dbias += in ? dv : 0.0f;
       }
     }
-    u_at.back(); dt_at.back(); z_at.back(); dy_at.back();
   }
   // behind a sample's end
   for (int t = max(t0, end) + lane / CW; t < t1; t += 64 / CW) {
