@@ -78,19 +78,19 @@ struct Cursor {
   uint32_t step;                       // bytes between rows
   __device__ __forceinline__ Cursor(const View<E>& v, int t, int b, int offset = 0)
       : base(reinterpret_cast<uint64_t>(v.data + ((int64_t)t * v.step + (int64_t)b * v.sample + offset))), step((uint32_t)v.step * (uint32_t)sizeof(E)) {}
-  // (width: elements of a row, 0 where there is no tensor.  FRESH: the compiler is to form offsets where they are used; kept
-  // for eight rows of seven tensors they fill the registers that the states of the backward pass are in.)
+  // (rows: 0 where there is no tensor.  FRESH: the compiler is to form offsets where they are used; kept for eight rows of
+  // seven tensors they fill the registers that the states of the backward pass are in.)
   template <bool FRESH = false>
   __device__ __forceinline__ Tile<E> tile(int rows, int width) const {
     rows = min(rows, kTile);
     uint32_t own_step = step;
     if (FRESH) asm volatile("" : "+s"(own_step));
-    const uint32_t bytes = width > 0 && rows > 0 ? (uint32_t)(rows - 1) * own_step + (uint32_t)width * (uint32_t)sizeof(E) : 0u;
+    const uint32_t bytes = rows > 0 ? (uint32_t)(rows - 1) * own_step + (uint32_t)width * (uint32_t)sizeof(E) : 0u;
     const uint64_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)base), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(base >> 32));
     return Tile<E>{__builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(lo | hi << 32), 0, __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000), own_step};
   }
-  __device__ __forceinline__ void forth() { base += (uint64_t)kTile * step; }
-  __device__ __forceinline__ void back() { base -= (uint64_t)kTile * step; }
+  __device__ __forceinline__ void forth() { base += (uint32_t)kTile * step; }    // (below 2^30)
+  __device__ __forceinline__ void back() { base -= (uint32_t)kTile * step; }
 };
 // One sample's states in this library's own layout, [quad][C][4]: an element's offset stays below 2^31 bytes.
 constexpr int kChannelsMost = 1 << 20;
@@ -102,12 +102,18 @@ struct States {
     const uint64_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32));
     buffer = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(lo | hi << 32), 0, base ? quads * channels * 16 : 0, 0x00020000);
   }
+  // the copy at an address, or none
+  __device__ __forceinline__ States(uint64_t at, int quads, int channels, bool there) : channels(channels) {
+    const uint64_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32));
+    buffer = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(lo | hi << 32), 0, there ? quads * channels * 16 : 0, 0x00020000);
+  }
   __device__ __forceinline__ floatx4_t load(int quad, int c) const {          // zeros behind the last quad
     return __builtin_bit_cast(floatx4_t, __builtin_amdgcn_raw_buffer_load_b128(buffer, (quad * channels + c) * 16, 0, 0));
   }
-  __device__ __forceinline__ void store(int quad, int c, const floatx4_t& v) const {
+  __device__ __forceinline__ void store(int quad, int c, const floatx4_t& v) const { store_at((quad * channels + c) * 16, v); }
+  __device__ __forceinline__ void store_at(int byte, const floatx4_t& v) const {
     typedef uint32_t words __attribute__((ext_vector_type(4)));
-    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(words, v), buffer, (quad * channels + c) * 16, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(words, v), buffer, byte, 0, 0);
   }
 };
 
@@ -130,6 +136,12 @@ __device__ __forceinline__ float softplus(float v) {
 constexpr float kRaise = 1.0e-8f;
 __device__ __forceinline__ float decay(float d, float A) { return exp2_fast(__builtin_fmaf(d, A, kRaise)); }
 
+// x y rounded: a product of its own can take x from another lane's register, a multiply-add can not.
+__device__ __forceinline__ float product(float x, float y) {
+#pragma clang fp contract(off)
+  return x * y;
+}
+
 // Step q's value out of S neighbouring lanes, of which lane q % S holds it.
 template <int S>
 __device__ __forceinline__ float from_owner(float v, int q) {
@@ -143,6 +155,27 @@ __device__ __forceinline__ float from_owner(float v, int q) {
                                      : q % 4 == 2 ? __builtin_amdgcn_mov_dpp(bits, 0xaa, 0xf, 0xf, true)
                                                   : __builtin_amdgcn_mov_dpp(bits, 0xff, 0xf, 0xf, true));
   else return __shfl(v, ((threadIdx.x & 63) & ~(S - 1)) | (q % S));
+}
+
+// (p, q): lanes without `BIT` get the sum of p over the two lanes that differ in BIT, the others that of q.
+template <int BIT>
+__device__ __forceinline__ float halve(float p, float q, int lane) {
+  if (BIT == 32 || BIT == 16) {
+    const uint32_t up = __builtin_bit_cast(uint32_t, p), uq = __builtin_bit_cast(uint32_t, q);
+    const auto r = BIT == 32 ? __builtin_amdgcn_permlane32_swap(up, uq, false, false) : __builtin_amdgcn_permlane16_swap(up, uq, false, false);
+    const uint32_t r0 = r[0], r1 = r[1];
+    return __builtin_bit_cast(float, r0) + __builtin_bit_cast(float, r1);
+  }
+  const bool upper = lane & BIT;
+  const float keep = upper ? q : p, give = upper ? p : q;
+  const int bits = __builtin_bit_cast(int, give);
+  if (BIT == 4) {   // from four lanes up in the lower halves of eight lanes, from four lanes down in the upper ones
+    const float up = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, bits, 0x104, 0xf, 0x5, false));
+    const float down = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, bits, 0x114, 0xf, 0xa, false));
+    return (keep + up) + down;
+  }
+  constexpr int kCtrl = BIT == 8 ? 0x128 : BIT == 2 ? 0x4e : 0xb1;   // row_ror 8, quad_perm 2 3 0 1, quad_perm 1 0 3 2
+  return keep + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(bits, kCtrl, 0xf, 0xf, true));
 }
 
 // The end states of segments 1.. (run from zero) chained into the true states in front of every segment:

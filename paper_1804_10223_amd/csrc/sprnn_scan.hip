@@ -79,7 +79,7 @@ __global__ __launch_bounds__(64 * S) void scan_kernel(ScanArgs a, View<const Ele
   Cursor<E> y_at(ys, t0, b);
   const bool gated = zs.data != nullptr;
   auto fetch = [&](Inputs& in, int rows) {
-    const Tile<const E> u_rows = u_at.tile(rows, a.C), dt_rows = dt_at.tile(rows, a.C), z_rows = z_at.tile(rows, gated ? a.C : 0);
+    const Tile<const E> u_rows = u_at.tile(rows, a.C), dt_rows = dt_at.tile(rows, a.C), z_rows = z_at.tile(gated ? rows : 0, a.C);
     const Tile<const E> B_rows = B_at.tile(rows, a.N), C_rows = C_at.tile(rows, a.N);
     u_at.forth(); dt_at.forth(); z_at.forth(); B_at.forth(); C_at.forth();
 #pragma unroll
@@ -96,6 +96,9 @@ __global__ __launch_bounds__(64 * S) void scan_kernel(ScanArgs a, View<const Ele
     }
   };
   float total = 0.0f;
+  uint64_t kept_at = reinterpret_cast<uint64_t>(kept) + ((int64_t)(t0 / kTile) * a.B + b) * a.quads * a.C * 16;
+  const uint64_t kept_step = (uint64_t)a.B * a.quads * a.C * 16;
+  const int kept_to = (sub * (NS / 4) * a.C + c) * 16;
   auto work = [&](Inputs& in, int t, int buffer) {           // one tile; its inputs are followed by those of kAhead tiles on
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
@@ -104,33 +107,33 @@ __global__ __launch_bounds__(64 * S) void scan_kernel(ScanArgs a, View<const Ele
       (&low[buffer][0][0][0])[at] = there ? (float)in.own_B[i] : 0.0f;
       if (!LOCAL) (&low[buffer][LOCAL ? 0 : 1][0][0])[at] = there ? (float)in.own_C[i] : 0.0f;
     }
-    if (MODE == kKeeping && mine && t < live) put_states(kept, t / kTile);
-    float d[kItems], x[kItems], gate[kItems], skip[kItems], y[kItems];
+    if (MODE == kKeeping) {
+      const States to(kept_at, a.quads, a.C, t < live);
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) d[i] = (float)in.dt[i] + bias;
-    if (a.softplus) {
-#pragma unroll
-      for (int i = 0; i < kItems; ++i) d[i] = softplus(d[i]);
+      for (int q = 0; q < NS / 4; ++q)
+        to.store_at(mine ? kept_to + q * a.C * 16 : -16, floatx4_t{h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]});   // (-16: nowhere)
+      kept_at += kept_step;
     }
+    float d[kItems], x[kItems], gate[kItems], skip[kItems];
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
       const bool there = t + i * S + sub < live;
-      const float ui = there ? (float)in.u[i] : 0.0f;
-      d[i] = there ? d[i] : 0.0f;
+      const float v = (float)in.dt[i] + bias, ui = there ? (float)in.u[i] : 0.0f;
+      float smooth = softplus(v);
+      asm volatile("" : "+v"(smooth));                     // selected, not branched around
+      d[i] = there ? a.softplus ? smooth : v : 0.0f;
       x[i] = d[i] * ui;
       skip[i] = D * ui;
       if (LOCAL) total += d[i];
-    }
-    if (!LOCAL) {
-#pragma unroll
-      for (int i = 0; i < kItems; ++i) gate[i] = 1.0f;
-      if (gated) {
-#pragma unroll
-        for (int i = 0; i < kItems; ++i) gate[i] = (float)in.z[i] * sigmoid((float)in.z[i]);
+      if (!LOCAL) {
+        float g = (float)in.z[i] * sigmoid((float)in.z[i]);
+        asm volatile("" : "+v"(g));
+        gate[i] = gated ? g : 1.0f;
       }
     }
     __syncthreads();
     fetch(in, live - t - kAhead * kTile);
+    float y[kTile];                                        // of step q; in a lane's first places of its own steps in the end
 #pragma unroll
     for (int q = 0; q < kTile; ++q) {
       const float* const Bq = &low[buffer][0][q][sub * NS];
@@ -139,14 +142,25 @@ __global__ __launch_bounds__(64 * S) void scan_kernel(ScanArgs a, View<const Ele
       float sum = 0.0f;
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
-        h[i] = decay(dq, A[i]) * h[i] + xq * Bq[i];
+        h[i] = __builtin_fmaf(decay(dq, A[i]), h[i], product(xq, Bq[i]));
         if (!LOCAL) sum += Cq[i] * h[i];
       }
       if (!LOCAL) {
-        sum = sum_lanes<S>(sum);
-        y[q / S] = S == 1 || sub == q % S ? sum : q % S ? y[q / S] : 0.0f;
-        if (S == 1) asm volatile("" : "+v"(y[q / S]));   // formed here, not where it is stored with all its factors alive till then
+        y[q] = S == 8 ? sum_lanes<S>(sum) : sum;
+        if (S == 1) asm volatile("" : "+v"(y[q]));         // formed here, not where it is stored with all its factors alive till then
       }
+    }
+    if (!LOCAL && (S == 2 || S == 4)) {                    // sums over a channel's lanes, each of which keeps its own steps'
+#pragma unroll
+      for (int q = 0; q < kTile / 2; ++q) y[q] = halve<1>(y[2 * q], y[2 * q + 1], tid);
+      if (S == 4) {
+#pragma unroll
+        for (int q = 0; q < kTile / 4; ++q) y[q] = halve<2>(y[2 * q], y[2 * q + 1], tid);
+      }
+    }
+    if (!LOCAL && S == 8) {
+#pragma unroll
+      for (int q = 1; q < kTile; ++q) y[0] = sub == q ? y[q] : y[0];
     }
     if (!LOCAL) {
       const Tile<E> y_rows = y_at.tile(live - t, a.C);

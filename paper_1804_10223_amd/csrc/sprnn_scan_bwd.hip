@@ -49,7 +49,7 @@ __global__ __launch_bounds__(64) void scan_adjoint_kernel(ScanArgs a, int segmen
   Cursor<const E> dy_at(dys, last, b), dt_at(dts, last, b), z_at(zs, last, b), C_at(Cs, last, b, group * a.N);
   const bool gated = zs.data != nullptr;
   auto fetch = [&](int rows) {
-    const Tile<const E> dy_rows = dy_at.tile(rows, a.C), dt_rows = dt_at.tile(rows, a.C), z_rows = z_at.tile(rows, gated ? a.C : 0), C_rows = C_at.tile(rows, a.N);
+    const Tile<const E> dy_rows = dy_at.tile(rows, a.C), dt_rows = dt_at.tile(rows, a.C), z_rows = z_at.tile(gated ? rows : 0, a.C), C_rows = C_at.tile(rows, a.N);
     dy_at.back(); dt_at.back(); z_at.back(); C_at.back();
 #pragma unroll
     for (int q = 0; q < kTile; ++q) {
@@ -94,27 +94,6 @@ __global__ __launch_bounds__(64) void scan_adjoint_kernel(ScanArgs a, int segmen
 #pragma unroll
   for (int q = 0; q < NS / 4; ++q) to.store(sub * (NS / 4) + q, c, floatx4_t{g[4 * q], g[4 * q + 1], g[4 * q + 2], g[4 * q + 3]});
   if (sub == 0) sums[((int64_t)slot * a.B + b) * a.C + c] = total;
-}
-
-// (p, q): lanes without `BIT` get the sum of p over the two lanes that differ in BIT, the others that of q.
-template <int BIT>
-__device__ __forceinline__ float halve(float p, float q, int lane) {
-  if (BIT == 32 || BIT == 16) {
-    const uint32_t up = __builtin_bit_cast(uint32_t, p), uq = __builtin_bit_cast(uint32_t, q);
-    const auto r = BIT == 32 ? __builtin_amdgcn_permlane32_swap(up, uq, false, false) : __builtin_amdgcn_permlane16_swap(up, uq, false, false);
-    const uint32_t r0 = r[0], r1 = r[1];
-    return __builtin_bit_cast(float, r0) + __builtin_bit_cast(float, r1);
-  }
-  const bool upper = lane & BIT;
-  const float keep = upper ? q : p, give = upper ? p : q;
-  const int bits = __builtin_bit_cast(int, give);
-  if (BIT == 4) {   // from four lanes up in the lower halves of eight lanes, from four lanes down in the upper ones
-    const float up = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, bits, 0x104, 0xf, 0x5, false));
-    const float down = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, bits, 0x114, 0xf, 0xa, false));
-    return (keep + up) + down;
-  }
-  constexpr int kCtrl = BIT == 8 ? 0x128 : BIT == 2 ? 0x4e : 0xb1;   // row_ror 8, quad_perm 2 3 0 1, quad_perm 1 0 3 2
-  return keep + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(bits, kCtrl, 0xf, 0xf, true));
 }
 
 constexpr int kSums = kTile * 8;       // numbers of a tile and quad: [step][dB, dC][state]
@@ -217,7 +196,7 @@ __global__ __launch_bounds__(64 * waves_of(S), 2) void scan_backward_kernel(Scan
   auto fetch_items = [&](Items& to, int rows) {
     load_items<CW>(to.u, u_at.template tile<true>(rows, a.C), lane, c_item);
     load_items<CW>(to.dt, dt_at.template tile<true>(rows, a.C), lane, c_item);
-    load_items<CW>(to.z, z_at.template tile<true>(rows, gated ? a.C : 0), lane, c_item);
+    load_items<CW>(to.z, z_at.template tile<true>(gated ? rows : 0, a.C), lane, c_item);
     load_items<CW>(to.dy, dy_at.template tile<true>(rows, a.C), lane, c_item);
   };
   constexpr int kLow = (kTile * kRow + 64 * W - 1) / (64 * W);
@@ -348,7 +327,7 @@ __global__ __launch_bounds__(64 * waves_of(S), 2) void scan_backward_kernel(Scan
       if (t + q < live) partial[((((int64_t)block * a.T + t + q) * a.B + b) * a.G + group) * (2 * kRow) + i % (2 * kRow)] = sum;
     }
     // gradients of what depends on (step, channel) alone
-    const Tile<E> du_rows = du_at.template tile<true>(live - t, io.du.data ? a.C : 0), ddt_rows = ddt_at.template tile<true>(live - t, io.ddt.data ? a.C : 0), dz_rows = dz_at.template tile<true>(live - t, io.dz.data ? a.C : 0);
+    const Tile<E> du_rows = du_at.template tile<true>(io.du.data ? live - t : 0, a.C), ddt_rows = ddt_at.template tile<true>(io.ddt.data ? live - t : 0, a.C), dz_rows = dz_at.template tile<true>(io.dz.data ? live - t : 0, a.C);
     du_at.back(); ddt_at.back(); dz_at.back();
     if (owned(item_channel)) {
       int rows = live - t;
