@@ -6,8 +6,8 @@
 // the exponential of a wavefront, 4 for each of the others.  So states live in registers, everything that depends on (step,
 // channel) alone is done once for all states of a channel, and steps are independent only through the state: where the
 // samples and channels are too few to fill the chip, time is divided into segments.  Segments but the last are run once from
-// a zero state for their effect (end state, sum of d: the product of all a of a state is exp(A sum d)), a small kernel
-// chains these, and a second run starts every segment from its true state.
+// a zero state for their effect (end state, sum of d: the product of all a of a state is exp(A sum d)), and a second run chains
+// these and starts every segment from its true state.
 #ifndef SPRNN_SCAN_H_
 #define SPRNN_SCAN_H_
 
@@ -36,6 +36,7 @@ ScanShape scan_shape(const sprnn_scan_t* p);
 
 struct ScanArgs {
   int T, B, C, N, G, per_group, blocks, quads, softplus;   // blocks: wavefronts per group of channels
+  int by_length;                       // workgroups are dealt out by their samples' lengths
   int segment;
   const float* A;
   const float* D;
@@ -43,7 +44,7 @@ struct ScanArgs {
   const int32_t* lengths;
 };
 inline ScanArgs scan_arguments(const sprnn_scan_t* p, const ScanShape& s) {
-  return ScanArgs{s.T, s.B, s.C, s.N, s.G, s.per_group, 0, s.quads, p->softplus, s.segment, p->A, p->D, p->dt_bias, p->lengths};
+  return ScanArgs{s.T, s.B, s.C, s.N, s.G, s.per_group, 0, s.quads, p->softplus, 0, s.segment, p->A, p->D, p->dt_bias, p->lengths};
 }
 bool good_scan(const sprnn_scan_t* p);
 
@@ -178,10 +179,40 @@ __device__ __forceinline__ float halve(float p, float q, int lane) {
   return keep + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(bits, kCtrl, 0xf, 0xf, true));
 }
 
-// The end states of segments 1.. (run from zero) chained into the true states in front of every segment:
-// H[0] = first, H[s + 1] += exp(A sums[s]) H[s].
-// (first: [B][C][N] as the callers have it, or null for zeros).
-hipError_t launch_chain(const ScanArgs& a, int segments, const float* first, float* H, const float* sums, hipStream_t stream);
+// The state in front of segment `seg` (of the adjoint: of the seg-th from the end).  The local runs left in H[0] the state in
+// front of the first segment, in H[1] the one behind it, and behind every other segment k what it makes of zero, H[k + 1], with
+// the sum of its d, sums[k]: h = exp(A sums[k]) h + H[k + 1] from there on.  Every workgroup of the second run does this for
+// itself, with four segments in flight: a launch in between took 8 us at 27 segments (1 x 4096 x 2304, 16 states).
+template <int Q>
+__device__ __forceinline__ void chained_states(float (&h)[4 * Q], const float (&A)[4 * Q], const ScanArgs& a, const float* H, const float* sums,
+                                               int seg, int b, int quad, int c) {
+  constexpr int kAhead = 4;
+  const States front(H, min(seg, 1), b, a.B, a.quads, a.C);
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    const floatx4_t p = front.load(quad + q, c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[4 * q + i] = p[i];
+  }
+  for (int s = 1; s < seg; s += kAhead) {
+    floatx4_t p[kAhead][Q];
+    float total[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int from = min(s + k, seg - 1);
+      const States behind(H, from + 1, b, a.B, a.quads, a.C);
+#pragma unroll
+      for (int q = 0; q < Q; ++q) p[k][q] = behind.load(quad + q, c);
+      total[k] = sums[((int64_t)from * a.B + b) * a.C + c];
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (s + k >= seg) break;
+#pragma unroll
+      for (int i = 0; i < 4 * Q; ++i) h[i] = __builtin_fmaf(exp2_fast(A[i] * total[k]), h[i], p[k][i / 4][i % 4]);
+    }
+  }
+}
 
 int64_t scan_backward_bytes(const ScanShape& s);
 hipError_t launch_scan_backward(const ScanShape& s, const sprnn_scan_t* p, const sprnn_seq_t& dy, const float* d_state_out, const float* kept,

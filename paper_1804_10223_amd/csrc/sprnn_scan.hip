@@ -9,12 +9,33 @@ namespace {
 
 int blocks_of(const ScanShape& s) { return (s.per_group + 63) / 64; }
 
+// Where all workgroups are resident from the start, a compute unit is as late as the sum of its samples is long.  Workgroups go
+// to the units in order, one to each before any gets its second: so the samples are taken from the longest on, and from the
+// shortest of the round on in every other round.  (8 x 2048 x 4608, lengths anywhere up to 2048: 309 us in the samples' order,
+// 279 from the longest on, 271 so.)
+constexpr int kUnits = kSimds / 4, kSamplesDealt = 64;
+__device__ __forceinline__ void deal_by_length(const ScanArgs& a, int& column, int& b) {
+  const int columns = gridDim.x, all = columns * a.B;
+  int at = blockIdx.y * columns + blockIdx.x;
+  const int round = at / kUnits;
+  if (round % 2 && (round + 1) * kUnits <= all) at = round * kUnits + (kUnits - 1 - at % kUnits);
+  const int wanted = at / columns, lane = threadIdx.x & 63;
+  column = at - wanted * columns;
+  const int own = lane < a.B ? sample_end(a.lengths, lane, a.T) : -1;
+  int rank = 0;                                            // samples in front of this lane's
+  for (int i = 0; i < a.B; ++i) {
+    const int other = __builtin_amdgcn_readlane(own, i);
+    rank += other > own || (other == own && i < lane);
+  }
+  b = __builtin_ctzll(__ballot(lane < a.B && rank == wanted));
+}
+
 // Prompts.  A workgroup owns 64 channels of one sample (and group) and a segment of time; S lanes share a channel, a lane
 // holds NS of its states, so there are S wavefronts.  Everything that depends on (step, channel) alone is computed once:
 // the S lanes of a channel share out the steps of a tile, and hand d and d u over to their neighbours.  B and C of a tile
 // are the same for all channels and are brought into LDS in binary32 once a tile; the next tile's loads are in flight while
 // a tile is worked through, and two LDS buffers make one barrier a tile enough.
-// kLocal: a segment's effect only (H[segment + 1] from a zero state, sums[segment] = sum of d).
+// kLocal: a segment's effect only (H[segment + 1] from a zero state, the first from its true one; sums[segment] = sum of d).
 enum { kPlain, kKeeping, kLocal };     // what a run of the forward pass leaves: y; y and the states in front of every tile; its effect
 
 template <int TYPE, int NS, int S, int MODE>
@@ -31,8 +52,10 @@ __global__ __launch_bounds__(64 * S) void scan_kernel(ScanArgs a, View<const Ele
   static_assert(S <= kTile && (kHalf || kTile * kN % (64 * S) == 0), "steps and states are dealt out evenly");
   __shared__ __attribute__((aligned(16))) float low[2][LOCAL ? 1 : 2][kTile][kN];
   const int tid = threadIdx.x, sub = tid % S;
-  const int group = blockIdx.x / a.blocks, block = blockIdx.x - group * a.blocks;
-  const int b = blockIdx.y, seg = blockIdx.z;
+  int column = blockIdx.x, b = blockIdx.y;
+  const int seg = blockIdx.z;
+  if (MODE != kLocal && a.by_length) deal_by_length(a, column, b);
+  const int group = column / a.blocks, block = column - group * a.blocks;
   const int in_group = block * 64 + tid / S;
   const bool mine = in_group < a.per_group;
   const int c = group * a.per_group + min(in_group, a.per_group - 1);
@@ -46,21 +69,13 @@ __global__ __launch_bounds__(64 * S) void scan_kernel(ScanArgs a, View<const Ele
     A[i] = n < a.N ? a.A[(int64_t)c * a.N + n] * kLog2e : 0.0f;
     h[i] = 0.0f;
   }
-  if (!LOCAL) {
-    if (H) {
-      const States from(H, seg, b, a.B, a.quads, a.C);
+  if (!LOCAL && H) {
+    chained_states<NS / 4>(h, A, a, H, sums, seg, b, sub * (NS / 4), c);
+  } else if (state_in && seg == 0) {
 #pragma unroll
-      for (int q = 0; q < NS / 4; ++q) {
-        const floatx4_t p = from.load(sub * (NS / 4) + q, c);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) h[4 * q + i] = p[i];
-      }
-    } else if (state_in) {
-#pragma unroll
-      for (int i = 0; i < NS; ++i) {
-        const int n = sub * NS + i;
-        if (n < a.N) h[i] = state_in[((int64_t)b * a.C + c) * a.N + n];
-      }
+    for (int i = 0; i < NS; ++i) {
+      const int n = sub * NS + i;
+      if (n < a.N) h[i] = state_in[((int64_t)b * a.C + c) * a.N + n];
     }
   }
   auto put_states = [&](float* base, int64_t copy) {
@@ -68,6 +83,7 @@ __global__ __launch_bounds__(64 * S) void scan_kernel(ScanArgs a, View<const Ele
 #pragma unroll
     for (int q = 0; q < NS / 4; ++q) to.store(sub * (NS / 4) + q, c, floatx4_t{h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]});
   };
+  if (LOCAL && seg == 0 && mine) put_states(H, 0);         // (the last segment may write its state over state_in)
   const float D = !LOCAL && a.D ? a.D[c] : 0.0f, bias = a.dt_bias ? a.dt_bias[c] : 0.0f;
 
   // this lane's steps of a tile are sub, sub + S, ..
@@ -199,44 +215,6 @@ __global__ __launch_bounds__(64 * S) void scan_kernel(ScanArgs a, View<const Ele
   }
 }
 
-// One lane per (sample, channel, quad of states).
-__global__ __launch_bounds__(64) void chain_kernel(ScanArgs a, int segments, const float* first, float* H, const float* sums) {
-  const int64_t at = (int64_t)blockIdx.x * 64 + threadIdx.x;
-  const int64_t lanes = (int64_t)a.B * a.quads * a.C;
-  if (at >= lanes) return;
-  const int c = (int)(at % a.C), quad = (int)(at / a.C % a.quads), b = (int)(at / ((int64_t)a.C * a.quads));
-  float A[4], h[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int n = quad * 4 + i;
-    A[i] = n < a.N ? a.A[(int64_t)c * a.N + n] * kLog2e : 0.0f;
-    h[i] = first && n < a.N ? first[((int64_t)b * a.C + c) * a.N + n] : 0.0f;
-  }
-  auto slot = [&](int s) { return H + ((int64_t)s * lanes + at) * 4; };
-  Pack<float, 4> front;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) front.v[i] = h[i];
-  store_pack(slot(0), front);
-  constexpr int kAhead = 8;                                // loads do not depend on the chain: eight segments in flight
-  for (int s = 1; s < segments; s += kAhead) {
-    Pack<float, 4> p[kAhead];
-    float total[kAhead];
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int from = min(s + k, segments - 1);
-      p[k] = load_pack<4>(slot(from));
-      total[k] = sums[((int64_t)(from - 1) * a.B + b) * a.C + c];
-    }
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      if (s + k >= segments) break;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) p[k].v[i] = h[i] = exp2_fast(A[i] * total[k]) * h[i] + p[k].v[i];
-      store_pack(slot(s + k), p[k]);
-    }
-  }
-}
-
 // Single tokens: the state is read and written once and bounds the call.  S lanes of four states a channel, so that a
 // wavefront's states are consecutive 16 bytes in memory; a lane reads its own part of everything.
 template <int TYPE, int S>
@@ -296,13 +274,12 @@ hipError_t run_prompt(ScanArgs a, const ScanShape& s, const sprnn_scan_t* p, con
   const View<const E> u = view<const E>(p->u), dt = view<const E>(p->dt), z = view<const E>(p->z), B = view<const E>(p->B), C = view<const E>(p->C);
   const dim3 block(64 * S);
   if (s.segments > 1) {
-    hipError_t e = launch(scan_kernel<TYPE, NS, S, kLocal>, dim3((unsigned)(a.blocks * s.G), (unsigned)s.B, (unsigned)s.segments - 1), block, 0, stream,
-                          a, u, dt, z, B, C, (const float*)nullptr, view<E>(y), (float*)nullptr, (float*)nullptr, H, sums);
-    if (e != hipSuccess) return e;
-    e = launch_chain(a, s.segments, state_in, H, sums, stream);
+    const hipError_t e = launch(scan_kernel<TYPE, NS, S, kLocal>, dim3((unsigned)(a.blocks * s.G), (unsigned)s.B, (unsigned)s.segments - 1), block, 0, stream,
+                          a, u, dt, z, B, C, state_in, view<E>(y), (float*)nullptr, (float*)nullptr, H, sums);
     if (e != hipSuccess) return e;
   } else {
     H = nullptr;
+    a.by_length = a.lengths && s.B > 1 && s.B <= kSamplesDealt;
   }
   return launch(kept ? scan_kernel<TYPE, NS, S, kKeeping> : scan_kernel<TYPE, NS, S, kPlain>, dim3((unsigned)(a.blocks * s.G), (unsigned)s.B, (unsigned)s.segments), block, 0, stream, a, u,
                 dt, z, B, C, state_in, view<E>(y), state_out, kept, H, sums);
@@ -337,11 +314,6 @@ int round_up(int n, int to) { return (n + to - 1) / to * to; }
 
 }  // namespace
 
-hipError_t launch_chain(const ScanArgs& a, int segments, const float* first, float* H, const float* sums, hipStream_t stream) {
-  const int64_t lanes = (int64_t)a.B * a.quads * a.C;
-  return launch(chain_kernel, dim3((unsigned)((lanes + 63) / 64)), dim3(64), 0, stream, a, segments, first, H, sums);
-}
-
 // How many lanes share a channel: as few as its states need (16 a lane at most), and more, down to four states a lane, while
 // there are fewer wavefronts than twice the SIMDs: sharing costs a tenth more instructions (8 x 2048 x 4608, 16 states: 850 us
 // with one lane a channel, 576 wavefronts).  Where that is not enough time is divided, which costs nearly twice the work.
@@ -365,7 +337,7 @@ ScanShape scan_shape(const sprnn_scan_t* p) {
     *segments = s.T > 0 ? (s.T + *segment - 1) / *segment : 1;
   };
   divide(columns * s.lanes, &s.segments, &s.segment);
-  divide(columns, &s.back_segments, &s.back_segment);
+  divide(2 * columns, &s.back_segments, &s.back_segment);
   return s;
 }
 

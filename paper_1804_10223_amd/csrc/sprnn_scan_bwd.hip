@@ -24,7 +24,7 @@ namespace {
 template <int TYPE, int NS, int S>
 __global__ __launch_bounds__(64) void scan_adjoint_kernel(ScanArgs a, int segments, View<const Element<TYPE>> dys,
                                                           View<const Element<TYPE>> dts, View<const Element<TYPE>> zs,
-                                                          View<const Element<TYPE>> Cs, float* H, float* sums) {
+                                                          View<const Element<TYPE>> Cs, const float* d_state_out, float* H, float* sums) {
   typedef Element<TYPE> E;
   constexpr int kRow = NS * S, kOwn = kTile * kRow / 64;
   static_assert(kTile * kRow % 64 == 0, "the tile's states are dealt out evenly");
@@ -41,8 +41,15 @@ __global__ __launch_bounds__(64) void scan_adjoint_kernel(ScanArgs a, int segmen
   for (int i = 0; i < NS; ++i) {
     const int n = sub * NS + i;
     A[i] = n < a.N ? a.A[(int64_t)c * a.N + n] * kLog2e : 0.0f;
-    g[i] = 0.0f;
+    g[i] = seg == segments - 1 && d_state_out && n < a.N ? d_state_out[((int64_t)b * a.C + c) * a.N + n] : 0.0f;
   }
+  const int slot = segments - 1 - seg;
+  auto put_states = [&](int copy) {
+    const States to(H, copy, b, a.B, a.quads, a.C);
+#pragma unroll
+    for (int q = 0; q < NS / 4; ++q) to.store(sub * (NS / 4) + q, c, floatx4_t{g[4 * q], g[4 * q + 1], g[4 * q + 2], g[4 * q + 3]});
+  };
+  if (slot == 0 && mine) put_states(0);
   const float bias = a.dt_bias ? a.dt_bias[c] : 0.0f;
   E dy[kTile], dt[kTile], z[kTile], own[kOwn];
   const int last = t0 + (live > t0 ? (live - t0 - 1) / kTile * kTile : 0);
@@ -89,10 +96,7 @@ __global__ __launch_bounds__(64) void scan_adjoint_kernel(ScanArgs a, int segmen
     }
   }
   if (!mine) return;
-  const int slot = segments - 1 - seg;
-  const States to(H, slot + 1, b, a.B, a.quads, a.C);
-#pragma unroll
-  for (int q = 0; q < NS / 4; ++q) to.store(sub * (NS / 4) + q, c, floatx4_t{g[4 * q], g[4 * q + 1], g[4 * q + 2], g[4 * q + 3]});
+  put_states(slot + 1);
   if (sub == 0) sums[((int64_t)slot * a.B + b) * a.C + c] = total;
 }
 
@@ -145,7 +149,7 @@ struct BackViews {
 // partial: [block of channels][T][B][groups][2][4 S] sums of dB and dC; totals: [segment][B][quads * C * 4 of dA, C of dD, C of d dt_bias].
 template <int TYPE, int S>
 __global__ __launch_bounds__(64 * waves_of(S), 2) void scan_backward_kernel(ScanArgs a, int segments, BackViews<TYPE> io, const float* kept,
-                                                                            const float* carry, const float* d_state_out, float* partial,
+                                                                            const float* carry, const float* carry_sums, const float* d_state_out, float* partial,
                                                                             float* totals, float* d_state) {
   typedef Element<TYPE> E;
   constexpr int W = waves_of(S), R = lane_channels(S), CW = wave_channels(S), CL = 64 / S;
@@ -165,18 +169,17 @@ __global__ __launch_bounds__(64 * waves_of(S), 2) void scan_backward_kernel(Scan
   auto owned = [&](int i) { return first + i < a.per_group; };
 
   float A[R][4], g[R][4], dA[R][4];
-  const States behind(carry, segments - 1 - seg, b, a.B, a.quads, a.C);
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int c = channel(r * CL + lane / S);
-    const floatx4_t p = behind.load(sub, c);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int n = sub * 4 + i;
       A[r][i] = n < a.N ? a.A[(int64_t)c * a.N + n] * kLog2e : 0.0f;
-      g[r][i] = carry ? p[i] : d_state_out && n < a.N ? d_state_out[((int64_t)b * a.C + c) * a.N + n] : 0.0f;
+      g[r][i] = !carry && d_state_out && n < a.N ? d_state_out[((int64_t)b * a.C + c) * a.N + n] : 0.0f;
       dA[r][i] = 0.0f;
     }
+    if (carry) chained_states<1>(g[r], A[r], a, carry, carry_sums, segments - 1 - seg, b, sub, c);
   }
   float dD = 0.0f, dbias = 0.0f;                             // of this lane's items, all of one channel
   const int item_channel = lane % CW, c_item = channel(item_channel);
@@ -465,15 +468,13 @@ hipError_t run(const ScanShape& s, const sprnn_scan_t* p, const sprnn_seq_t& dy,
     if (s.back_segments > 1) {
       a.blocks = (s.per_group + 64 / SA - 1) / (64 / SA);
       e = launch(scan_adjoint_kernel<TYPE, NS, SA>, dim3((unsigned)(a.blocks * s.G), (unsigned)s.B, (unsigned)s.back_segments - 1), dim3(64), 0, stream, a,
-                 s.back_segments, io.dy, io.dt, io.z, io.C, workspace + w.carry, workspace + w.sums);
-      if (e != hipSuccess) return e;
-      e = launch_chain(a, s.back_segments, d_state_out, workspace + w.carry, workspace + w.sums, stream);
+                 s.back_segments, io.dy, io.dt, io.z, io.C, d_state_out, workspace + w.carry, workspace + w.sums);
       if (e != hipSuccess) return e;
       carry = workspace + w.carry;
     }
     a.blocks = blocks_of(s, S);
     e = launch(scan_backward_kernel<TYPE, S>, dim3((unsigned)(a.blocks * s.G), (unsigned)s.B, (unsigned)s.back_segments), dim3(64 * waves_of(S)), 0, stream, a,
-               s.back_segments, io, kept, carry, d_state_out, workspace + w.partial, workspace + w.totals, out->state);
+               s.back_segments, io, kept, carry, (const float*)(workspace + w.sums), d_state_out, workspace + w.partial, workspace + w.totals, out->state);
     if (e != hipSuccess) return e;
     const int64_t lows = (int64_t)s.T * s.B * s.G * 8 * S;
     if (lows > 0 && (out->B.data || out->C.data)) {
