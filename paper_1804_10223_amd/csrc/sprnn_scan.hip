@@ -190,7 +190,10 @@ __global__ __launch_bounds__(64 * S) void scan_kernel(ScanArgs a, View<const Ele
   // A tile takes a wavefront about as long as a load from memory when few wavefronts share a SIMD.
   Inputs ring[kAhead];
 #pragma unroll
-  for (int k = 0; k < kAhead; ++k) fetch(ring[k], live - t0 - k * kTile);
+  for (int k = 0; k < kAhead; ++k) {
+    fetch(ring[k], live - t0 - k * kTile);
+    __builtin_amdgcn_sched_barrier(0);                     // in this order, or the loop's waits for one are waits for all
+  }
   // (whole rounds of kAhead tiles, without a branch that a load in flight would have to be waited for: tiles behind the end
   // multiply the states by one and store nothing)
   for (int t = t0; t < live; t += kAhead * kTile) {

@@ -20,18 +20,19 @@
 namespace sprnn {
 namespace {
 
-// A segment's effect on the adjoint, from zero behind it: like the forward pass's, from the end.
+// A segment's effect on the adjoint, from zero behind it: like the forward pass's, from the end.  One wavefront a workgroup,
+// S lanes a channel, which share out the steps of a tile; the next tile's loads are in flight while a tile is worked through.
 template <int TYPE, int NS, int S>
 __global__ __launch_bounds__(64) void scan_adjoint_kernel(ScanArgs a, int segments, View<const Element<TYPE>> dys,
                                                           View<const Element<TYPE>> dts, View<const Element<TYPE>> zs,
                                                           View<const Element<TYPE>> Cs, const float* d_state_out, float* H, float* sums) {
   typedef Element<TYPE> E;
-  constexpr int kRow = NS * S, kOwn = kTile * kRow / 64;
-  static_assert(kTile * kRow % 64 == 0, "the tile's states are dealt out evenly");
+  constexpr int kRow = NS * S, kOwn = kTile * kRow / 64, kItems = kTile / S;
+  static_assert(kTile * kRow % 64 == 0 && kTile % S == 0, "the tile's states and steps are dealt out evenly");
   __shared__ __attribute__((aligned(16))) float low[2][kTile][kRow];
   const int lane = threadIdx.x, sub = lane % S;
   const int group = blockIdx.x / a.blocks, block = blockIdx.x - group * a.blocks;
-  const int b = blockIdx.y, seg = blockIdx.z + 1;         // nothing asks for the effect of the first one
+  const int b = blockIdx.y, seg = blockIdx.z + 1, slot = segments - 1 - seg;         // nothing asks for the effect of the first one
   const int in_group = block * (64 / S) + lane / S;
   const bool mine = in_group < a.per_group;
   const int c = group * a.per_group + min(in_group, a.per_group - 1);
@@ -41,9 +42,8 @@ __global__ __launch_bounds__(64) void scan_adjoint_kernel(ScanArgs a, int segmen
   for (int i = 0; i < NS; ++i) {
     const int n = sub * NS + i;
     A[i] = n < a.N ? a.A[(int64_t)c * a.N + n] * kLog2e : 0.0f;
-    g[i] = seg == segments - 1 && d_state_out && n < a.N ? d_state_out[((int64_t)b * a.C + c) * a.N + n] : 0.0f;
+    g[i] = slot == 0 && d_state_out && n < a.N ? d_state_out[((int64_t)b * a.C + c) * a.N + n] : 0.0f;
   }
-  const int slot = segments - 1 - seg;
   auto put_states = [&](int copy) {
     const States to(H, copy, b, a.B, a.quads, a.C);
 #pragma unroll
@@ -51,50 +51,65 @@ __global__ __launch_bounds__(64) void scan_adjoint_kernel(ScanArgs a, int segmen
   };
   if (slot == 0 && mine) put_states(0);
   const float bias = a.dt_bias ? a.dt_bias[c] : 0.0f;
-  E dy[kTile], dt[kTile], z[kTile], own[kOwn];
+  struct Inputs {
+    E dy[kItems], dt[kItems], z[kItems], own[kOwn];
+  };
   const int last = t0 + (live > t0 ? (live - t0 - 1) / kTile * kTile : 0);
   Cursor<const E> dy_at(dys, last, b), dt_at(dts, last, b), z_at(zs, last, b), C_at(Cs, last, b, group * a.N);
   const bool gated = zs.data != nullptr;
-  auto fetch = [&](int rows) {
+  auto fetch = [&](Inputs& in, int rows) {
     const Tile<const E> dy_rows = dy_at.tile(rows, a.C), dt_rows = dt_at.tile(rows, a.C), z_rows = z_at.tile(gated ? rows : 0, a.C), C_rows = C_at.tile(rows, a.N);
     dy_at.back(); dt_at.back(); z_at.back(); C_at.back();
 #pragma unroll
-    for (int q = 0; q < kTile; ++q) {
-      dy[q] = dy_rows.load(q, c);
-      dt[q] = dt_rows.load(q, c);
-      z[q] = z_rows.load(q, c);
+    for (int i = 0; i < kItems; ++i) {
+      in.dy[i] = dy_rows.load(i * S + sub, c);
+      in.dt[i] = dt_rows.load(i * S + sub, c);
+      in.z[i] = z_rows.load(i * S + sub, c);
     }
 #pragma unroll
-    for (int i = 0; i < kOwn; ++i) own[i] = C_rows.load((i * 64 + lane) / kRow, (i * 64 + lane) % kRow);
+    for (int i = 0; i < kOwn; ++i) in.own[i] = C_rows.load((i * 64 + lane) / kRow, (i * 64 + lane) % kRow);
   };
-  float total = 0.0f;
-  fetch(live - last);
-  int buffer = 0;
-  for (int t = last; t >= t0 && live > t0; t -= kTile, buffer ^= 1) {
+  float total = 0.0f, behind = 0.0f;                       // g_t = a_{t+1} g_{t+1} + C_t e_t takes its factor from the step behind
+  auto work = [&](Inputs& in, int t, int buffer) {
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
       const int at = i * 64 + lane;
-      (&low[buffer][0][0])[at] = at % kRow < a.N && t + at / kRow < live ? (float)own[i] : 0.0f;
+      (&low[buffer][0][0])[at] = at % kRow < a.N && t + at / kRow < live ? (float)in.own[i] : 0.0f;
     }
-    float d[kTile], e[kTile];
+    float d[kItems], e[kItems];
 #pragma unroll
-    for (int q = 0; q < kTile; ++q) {
-      const float v = (float)dt[q] + bias, gate = (float)z[q];
-      const bool in = t + q < live;
-      d[q] = in ? a.softplus ? softplus(v) : v : 0.0f;
-      e[q] = in ? (float)dy[q] * (gated ? gate * sigmoid(gate) : 1.0f) : 0.0f;
+    for (int i = 0; i < kItems; ++i) {
+      const bool there = t >= t0 && t + i * S + sub < live;
+      const float v = (float)in.dt[i] + bias, z = (float)in.z[i];
+      float smooth = softplus(v), gate = z * sigmoid(z);
+      asm volatile("" : "+v"(smooth), "+v"(gate));         // selected, not branched around
+      d[i] = there ? a.softplus ? smooth : v : 0.0f;
+      e[i] = there ? (float)in.dy[i] * (gated ? gate : 1.0f) : 0.0f;
+      total += d[i];
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    fetch(t > t0 ? kTile : 0);
+    fetch(in, t - 2 * kTile >= t0 ? kTile : 0);
 #pragma unroll
     for (int q = kTile - 1; q >= 0; --q) {
+      const float dq = from_owner<S>(d[q / S], q), eq = from_owner<S>(e[q / S], q);
 #pragma unroll
-      for (int i = 0; i < NS; ++i) g[i] = decay(d[q], A[i]) * (g[i] + low[buffer][q][sub * NS + i] * e[q]);
-      total += d[q];
+      for (int i = 0; i < NS; ++i) g[i] = __builtin_fmaf(decay(behind, A[i]), g[i], product(eq, low[buffer][q][sub * NS + i]));
+      behind = dq;
     }
+  };
+  Inputs even, odd;                                        // in turn; a tile in front of the segment multiplies by one
+  fetch(even, live - last);
+  __builtin_amdgcn_sched_barrier(0);                       // in this order, or the loop's waits for one are waits for both
+  fetch(odd, last > t0 ? kTile : 0);
+  for (int t = last; t >= t0 && live > t0; t -= 2 * kTile) {
+    work(even, t, 0);
+    work(odd, t - kTile, 1);
   }
+#pragma unroll
+  for (int i = 0; i < NS; ++i) g[i] *= decay(behind, A[i]);
+  total = sum_lanes<S>(total);
   if (!mine) return;
   put_states(slot + 1);
   if (sub == 0) sums[((int64_t)slot * a.B + b) * a.C + c] = total;
@@ -491,10 +506,10 @@ hipError_t run(const ScanShape& s, const sprnn_scan_t* p, const sprnn_seq_t& dy,
 template <int TYPE>
 hipError_t run_backward(const ScanShape& s, const sprnn_scan_t* p, const sprnn_seq_t& dy, const float* d_state_out, const float* kept,
                         const sprnn_scan_gradients_t* out, float* workspace, hipStream_t stream) {
-  return s.N <= 4 ? run<TYPE, 8, 1, 1>(s, p, dy, d_state_out, kept, out, workspace, stream)
-       : s.N <= 8 ? run<TYPE, 8, 1, 2>(s, p, dy, d_state_out, kept, out, workspace, stream)
-       : s.N <= 16 ? run<TYPE, 16, 1, 4>(s, p, dy, d_state_out, kept, out, workspace, stream)
-       : s.N <= 32 ? run<TYPE, 16, 2, 8>(s, p, dy, d_state_out, kept, out, workspace, stream)
+  return s.N <= 4 ? run<TYPE, 4, 2, 1>(s, p, dy, d_state_out, kept, out, workspace, stream)
+       : s.N <= 8 ? run<TYPE, 4, 2, 2>(s, p, dy, d_state_out, kept, out, workspace, stream)
+       : s.N <= 16 ? run<TYPE, 4, 4, 4>(s, p, dy, d_state_out, kept, out, workspace, stream)
+       : s.N <= 32 ? run<TYPE, 8, 4, 8>(s, p, dy, d_state_out, kept, out, workspace, stream)
        : s.N <= 64 ? run<TYPE, 16, 4, 16>(s, p, dy, d_state_out, kept, out, workspace, stream)
                    : run<TYPE, 16, 8, 32>(s, p, dy, d_state_out, kept, out, workspace, stream);
 }
