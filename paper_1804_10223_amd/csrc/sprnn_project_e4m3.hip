@@ -294,6 +294,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(ProductArgs
 // 128 conversions (5 cycles) and 64 scaled sums; the widened fragments and the running sums fill the registers (IR = 4 is 27
 // too many).  On e4m3 itself the fragments are a quarter of that, and 128 x 64 outputs a wavefront halve what LDS has to
 // deliver for a matrix instruction.
+// Where a CU has one workgroup, one wavefront a SIMD would go through loads from LDS, products and sums one after the other:
+// KS = 2 gives a workgroup a second set of wavefronts and stages for every other slab, and the two sums meet in the end.
 // Measured on 8192 x 2304 x 9216: float32 430 us (matrix instructions 139 us of it at 2.4 GHz; the chip runs at 2.0 here),
 // bfloat16 220.  Of the float32 form, others came out within 5 % (eight wavefronts and three stages 425, half slabs in five
 // stages 470), and widening once a workgroup, on the way into LDS, at 500: twice the bytes through LDS.
@@ -303,7 +305,8 @@ template <> struct Many<4> { static constexpr int kWR = 2, kWM = 4; };
 template <int IR> constexpr int many_r() { return Many<IR>::kWR * IR * 32; }
 template <int IR> constexpr int many_m() { return Many<IR>::kWM * 64; }
 template <int IR> constexpr int many_threads() { return Many<IR>::kWR * Many<IR>::kWM * 64; }
-template <int IR> constexpr int many_stage() { return (many_r<IR>() + many_m<IR>()) * kSlab; }
+template <int IR> constexpr int many_rows() { return (many_r<IR>() + many_m<IR>()) * kSlab; }          // bytes of a slab's rows
+template <int IR> constexpr int many_stage() { return many_rows<IR>() + many_threads<IR>() * 8; }       // ... and its scales
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 // 32 rows of a slab: this lane's four pieces, every other one of its row.
@@ -336,15 +339,16 @@ __device__ __forceinline__ floatx16 multiply(const Strip<true>& w, const Strip<t
   return c;
 }
 
-template <int TYPE, int IR>
-__global__ __launch_bounds__(many_threads<IR>(), 2) void product_many_kernel(ProductArgs a, Element<TYPE>* out) {
+template <int TYPE, int IR, int KS>
+__global__ __launch_bounds__(many_threads<IR>() * KS, 2) void product_many_kernel(ProductArgs a, Element<TYPE>* out) {
   constexpr bool kWide = TYPE == SPRNN_TYPE_F32;
   constexpr int WR = Many<IR>::kWR, kM = many_m<IR>(), kR = many_r<IR>();
   constexpr int kWaves = many_threads<IR>() / 64, kCopiesM = kM / (kWaves * 8), kCopiesR = kR / (kWaves * 8);
   static_assert(kWaves * 8 % 16 == 0, "a lane fetches the same piece of all its rows");
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) % kWaves, part = __builtin_amdgcn_readfirstlane(tid >> 6) / kWaves;
+  uint8_t* const own_lds = lds + part * 2 * many_stage<IR>();
   // Workgroups go to the eight XCDs in turn: each gets a run of tiles, eight along m by a few along r at a time, whose rows
   // its L2 holds.
   const int nb = gridDim.x, bid = blockIdx.x;
@@ -365,19 +369,29 @@ __global__ __launch_bounds__(many_threads<IR>(), 2) void product_many_kernel(Pro
   }
 #pragma unroll
   for (int i = 0; i < kCopiesR; ++i) w_at[i] = a.w + (int64_t)min(r0 + i * kWaves * 8 + own_row, a.rows - 1) * a.inputs + piece;
+  typedef const __attribute__((address_space(1))) void* Global;
+  typedef __attribute__((address_space(3))) void* Local;
   auto bring = [&](const uint8_t* from, uint8_t* to) {
-    typedef const __attribute__((address_space(1))) void* Global;
-    typedef __attribute__((address_space(3))) void* Local;
+    asm volatile("" : "+v"(from));               // one copy whatever the address, no branch
     __builtin_amdgcn_global_load_lds((Global)from, (Local)to, 16, 0, 0);
   };
+  const int wr = wave % WR * (IR * 32), wm = wave / WR * 64;
+  const float* const x_scale = a.x_scales + min(m0 + wm + lane, a.vectors - 1) * a.blocks;
+  const float* const w_scale = a.w_scales + (int64_t)min((r0 + wr) / 128, (a.rows - 1) / 128) * a.blocks;
   auto copy = [&](int slab, int at) {
-    uint8_t* const to = lds + at * many_stage<IR>() + wave * 8 * kSlab;
+    uint8_t* const stage = own_lds + at * many_stage<IR>();
+    uint8_t* const to = stage + wave * 8 * kSlab;
     const int64_t k = (int64_t)slab * kSlab;
     const bool there = k + piece < a.inputs;     // pieces are whole: the rows' length is a multiple of 16
 #pragma unroll
     for (int i = 0; i < kCopiesM; ++i) bring(there ? x_at[i] + k : nothing, to + i * kWaves * 8 * kSlab);
 #pragma unroll
     for (int i = 0; i < kCopiesR; ++i) bring(there ? w_at[i] + k : nothing, to + (kM + i * kWaves * 8) * kSlab);
+    // the scales of this wavefront's 64 rows of x, and 64 times that of its rows of w
+    uint8_t* const scales = stage + many_rows<IR>() + wave * 512;
+    const int from = min(slab, a.blocks - 1);
+    __builtin_amdgcn_global_load_lds((Global)(x_scale + from), (Local)scales, 4, 0, 0);
+    __builtin_amdgcn_global_load_lds((Global)(w_scale + from), (Local)(scales + 256), 4, 0, 0);
   };
   // The copies have no registers that the compiler would wait for: every wavefront waits for its own, and for its reads of
   // the slab that the next copies replace.
@@ -388,12 +402,7 @@ __global__ __launch_bounds__(many_threads<IR>(), 2) void product_many_kernel(Pro
     asm volatile("" ::: "memory");
   };
 
-  const int wr = wave % WR * (IR * 32), wm = wave / WR * 64;
   const int fr = lane & 31, half = lane >> 5;
-  const float* scale_row[2];
-#pragma unroll
-  for (int j = 0; j < 2; ++j) scale_row[j] = a.x_scales + min(m0 + wm + j * 32 + fr, a.vectors - 1) * a.blocks;
-  const float* const w_scale = a.w_scales + (int64_t)min((r0 + wr) / 128, (a.rows - 1) / 128) * a.blocks;
   floatx16 acc[IR][2];
 #pragma unroll
   for (int i = 0; i < IR; ++i)
@@ -404,15 +413,19 @@ __global__ __launch_bounds__(many_threads<IR>(), 2) void product_many_kernel(Pro
 #pragma unroll
     for (int i = 0; i < 4; ++i) f.set(i, *reinterpret_cast<const uint4*>(tile + piece_at(row, 2 * i + half)));
   };
-  float s[2] = {scale_row[0][0] * w_scale[0], scale_row[1][0] * w_scale[0]};
-  copy(0, 0);
+  copy(part, 0);
   next_slab();
-  for (int slab = 0; slab < a.blocks; ++slab) {
-    const uint8_t* const xs = lds + (slab & 1) * many_stage<IR>();
+  for (int first = 0, at = 0; first < a.blocks; first += KS, at ^= 1) {
+    const int slab = first + part;
+    const uint8_t* const xs = own_lds + at * many_stage<IR>();
     const uint8_t* const ws = xs + kM * kSlab;
-    const int next = min(slab + 1, a.blocks - 1);
-    const float s0 = scale_row[0][next], s1 = scale_row[1][next], w0 = w_scale[next];
-    copy(slab + 1, (slab + 1) & 1);              // (zeros behind the last one)
+    copy(slab + KS, at ^ 1);                     // (zeros behind the last one)
+    if (KS > 1 && slab >= a.blocks) {
+      next_slab();
+      continue;
+    }
+    const float* const scales = reinterpret_cast<const float*>(xs + many_rows<IR>() + wave * 512);
+    const float s[2] = {scales[fr] * scales[64], scales[32 + fr] * scales[64]};
     Strip<kWide> xf[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) strip(xf[j], xs, wm + j * 32 + fr);
@@ -428,14 +441,34 @@ __global__ __launch_bounds__(many_threads<IR>(), 2) void product_many_kernel(Pro
       }
     }
     next_slab();
-    s[0] = s0 * w0;
-    s[1] = s1 * w0;
+  }
+  uint8_t* free_lds = lds;
+  if (KS > 1) {                                  // the parts of the slabs meet
+    floatx4* const meet = reinterpret_cast<floatx4*>(lds) + wave * 64 + lane;
+    constexpr int kMeet = kWaves * 64;
+    static_assert(KS == 1 || (KS == 2 && IR * 2 * 4 * kMeet * 16 + kWaves * 32 * 68 * 4 <= 4 * many_stage<IR>()), "the other part's sums and the turns fit");
+    if (part == 1) {
+#pragma unroll
+      for (int i = 0; i < IR * 2 * 4; ++i) {
+        const floatx16& t = acc[i / 8][i / 4 % 2];
+        meet[i * kMeet] = floatx4{t[4 * (i % 4)], t[4 * (i % 4) + 1], t[4 * (i % 4) + 2], t[4 * (i % 4) + 3]};
+      }
+    }
+    __syncthreads();
+    if (part == 1) return;
+#pragma unroll
+    for (int i = 0; i < IR * 2 * 4; ++i) {
+      const floatx4 other = meet[i * kMeet];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) acc[i / 8][i / 4 % 2][4 * (i % 4) + v] += other[v];
+    }
+    free_lds += IR * 2 * 4 * kMeet * 16;
   }
   // Sums leave through LDS: a lane has four neighbouring outputs of a row, 32 bytes of it a store with its neighbour.  A
   // wavefront turns its own tiles, 32 rows of x by 64 of w at a time, and stores rows of 64 outputs.
   constexpr int kPitch = 64 + 4;                 // floats; four more keep the rows of a turn off each other's banks
   static_assert(kWaves * 32 * kPitch * 4 <= 2 * many_stage<IR>(), "a turn of every wavefront fits");
-  float* const turn = reinterpret_cast<float*>(lds) + wave * 32 * kPitch;
+  float* const turn = reinterpret_cast<float*>(free_lds) + wave * 32 * kPitch;
   auto in_order = [] {                           // LDS serves a wavefront in order; the compiler is to keep it
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -473,8 +506,10 @@ template <int TYPE>
 hipError_t run_product(ProductArgs a, const sprnn_seq_t& out, hipStream_t stream) {
   Element<TYPE>* const to = static_cast<Element<TYPE>*>(out.data);
   auto groups = [&](int m, int r) { return (a.vectors + m - 1) / m * ((a.rows + r - 1) / r); };
-  // Few rows, or outputs of fewer 128 x 128 tiles than half of the CUs.
-  if (a.vectors <= 64 || groups(kTileM, kTileR) < 128) {
+  // Few rows, or outputs of fewer 128 x 128 tiles than a quarter of the CUs (tiles at 128 x 2304 x 9216, 72 of them: 20 us,
+  // the few rows' kernel 26; at 768 x 5120 x 2560, 120, 40 and 78; at 256 x 5120 x 2560, 40, both 40; at 128 x 1024 x 4096, 32,
+  // 11 and 7).
+  if (a.vectors <= 64 || groups(kTileM, kTileR) < 64) {
     const int rows = a.vectors <= 16 ? 16 : a.vectors <= 32 ? 32 : 64;
     auto kernel = a.inputs % 16 == 0 ? rows == 16   ? product_few_kernel<TYPE, 1, 1, true>
                                        : rows == 32 ? product_few_kernel<TYPE, 2, 2, true>
@@ -495,10 +530,16 @@ hipError_t run_product(ProductArgs a, const sprnn_seq_t& out, hipStream_t stream
       return launch(kernel, dim3((unsigned)n), dim3((unsigned)threads), lds, stream, a, to);
     };
     if constexpr (TYPE != SPRNN_TYPE_F32) {
-      if (groups(many_m<4>(), many_r<4>()) >= 192)
-        return run(product_many_kernel<TYPE, 4>, many_m<4>(), many_r<4>(), many_threads<4>(), 2 * many_stage<4>());
+      // Tiles of 256 x 256, one to a CU at a time, unless the last round of them leaves too many CUs idle (288 tiles at
+      // 2048 x 2304 x 9216: 82 us, 128 x 128 78).
+      const int64_t tiles = groups(many_m<4>(), many_r<4>()), rounds = (tiles + 255) / 256;
+      if (10 * tiles >= 7 * 256 * rounds)
+        return run(product_many_kernel<TYPE, 4, 1>, many_m<4>(), many_r<4>(), many_threads<4>(), 2 * many_stage<4>());
     }
-    return run(product_many_kernel<TYPE, 2>, many_m<2>(), many_r<2>(), many_threads<2>(), 2 * many_stage<2>());
+    // One workgroup to a CU or less: two halves of the slabs side by side (256 x 2304 x 9216, 144 tiles: 20 us, one 23).
+    if (groups(many_m<2>(), many_r<2>()) <= 256)
+      return run(product_many_kernel<TYPE, 2, 2>, many_m<2>(), many_r<2>(), 2 * many_threads<2>(), 4 * many_stage<2>());
+    return run(product_many_kernel<TYPE, 2, 1>, many_m<2>(), many_r<2>(), many_threads<2>(), 2 * many_stage<2>());
   }
   a.tiles_m = (int)((a.vectors + kTileM - 1) / kTileM);
   const int64_t tiles = groups(kTileM, kTileR);

@@ -154,6 +154,7 @@ def _sizes(function, head, count):
 
 # ------------------------------------------------------------------------------------------------------- selective scan
 
+@functools.lru_cache(maxsize=256)
 def scan_sizes(steps, batch, channels, states, groups=1):
     """sprnn_scan_sizes: bytes of (forward workspace, backward workspace, what the forward pass keeps)."""
     return _sizes("sprnn_scan_sizes", _SCAN.pack(steps, batch, channels, states, groups, *([0] * 21)), 3)
