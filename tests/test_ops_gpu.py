@@ -107,6 +107,11 @@ SCANS = [
     (515, 1, 100, 3, 1, "bf16", True, True, True, True, True, None, "slice"),
     (600, 1, 17, 40, 1, "f32", True, True, True, True, True, [0], "batch"),
     (300, 3, 10, 8, 2, "f32", False, True, False, False, False, [300, 1, 64], "time"),
+    (1100, 1, 40, 16, 1, "f32", True, True, True, True, True, [900], "time"),
+    (1000, 2, 9, 4, 1, "f16", True, True, True, True, True, None, "batch"),
+    # samples dealt out by their lengths, more workgroups than two for every compute unit; more samples than are dealt
+    (6, 9, 4100, 4, 1, "bf16", True, True, True, True, True, [6, 0, 3, 1, 5, 6, 2, 4, 6], "time"),
+    (5, 70, 66, 3, 2, "f32", True, True, True, True, True, [i % 7 for i in range(70)], "batch"),
 ]
 
 
@@ -308,6 +313,11 @@ NORMS = [
     (2, 1, 8200, "f32", "f32", True, "slice"),
     (1, 2, 16389, "bf16", "f32", True, "time"),
     (2, 1, 40001, "f16", "f16", True, "time"),
+    (2, 3, 16384, "bf16", "f32", True, "time"),
+    # several rows a workgroup, aligned and not
+    (1300, 5, 1032, "bf16", "f32", True, "batch"),
+    (1300, 4, 1031, "bf16", "f32", True, "slice"),
+    (2900, 3, 512, "f16", "f16", True, "time"),
 ]
 
 
@@ -417,6 +427,11 @@ PROJECTS = [
     (875, 4, 144, 3601, "bf16", True, "time"),
     (1000, 4, 128, 3073, "f16", True, "time"),
     (450, 8, 368, 3400, "bf16", False, "batch"),
+    # 128 x 128 tiles, one to a compute unit: an even, an odd and a single number of blocks
+    (20, 8, 2304, 5800, "bf16", True, "time"),
+    (30, 5, 400, 8300, "f32", True, "batch"),
+    (9, 33, 336, 3900, "f16", False, "time"),
+    (100, 1, 64, 8200, "bf16", True, "time"),
 ]
 
 
