@@ -5,10 +5,11 @@
 //
 // Bound by bytes: x is read and y written once.  A lane owns V neighbouring channels (8 bytes of them, at any alignment) and
 // walks a stretch of time with the last K - 1 inputs in registers, four rows in flight while four are worked on.  8 x 2048 x
-// 4608 in bfloat16: 70 us, 4.3 TB/s; with 16 bytes a lane 101 (three wavefronts a SIMD), with eight rows fetched and then
-// worked on 95.  Backward 8 x 1024 x 2048: 42 us, twice what its bytes take: the vector units work on 35 numbers a step and
-// channel (p again, the sigmoid, both gradients) and on K - 1 steps more for every stretch of 32.  The state of the K - 1 inputs before the call is read and written by the lanes of the first stretch alone:
-// it may be updated in place.
+// 4608 in bfloat16: 61 us, 4.9 TB/s; with 16 bytes a lane three wavefronts a SIMD are left (101 us against 70 at the time), and
+// eight rows fetched and then worked on took 95.  Backward 8 x 1024 x 2048: 32 us and 4 for the parameters' sums, 21 by its
+// bytes: the vector units work on 35 numbers a step and channel (p again, the sigmoid, both gradients), and on K - 1 steps more
+// for every stretch of 32 (stretches of 64, 40 us: half as many wavefronts).  The state of the K - 1 inputs before the call is
+// read and written by the lanes of the first stretch alone: it may be updated in place.
 #include "sprnn_sums.h"
 
 namespace sprnn {
@@ -25,17 +26,18 @@ struct ConvArgs {
   const int32_t* lengths;
 };
 
-template <typename E, int V>
+// WHOLE: the channels are a multiple of V, so that no load stands under a branch, which would be waited for where it ends.
+template <typename E, int V, bool WHOLE = false>
 __device__ __forceinline__ Pack<E, V> load_channels(const E* row, int c, int C) {
-  if (c + V <= C) return load_pack<V>(row + c);
+  if (WHOLE || c + V <= C) return load_pack<V>(row + c);
   return load_part<V>(row + c, C - c);
 }
-template <typename E, int V>
+template <typename E, int V, bool WHOLE = false>
 __device__ __forceinline__ void store_channels(E* row, int c, int C, const float (&f)[V]) {
   Pack<E, V> p;
 #pragma unroll
   for (int i = 0; i < V; ++i) p.v[i] = (E)f[i];
-  if (c + V <= C) store_pack(row + c, p);
+  if (WHOLE || c + V <= C) store_pack(row + c, p);
   else store_part(row + c, p, C - c);
 }
 
@@ -76,7 +78,7 @@ __device__ __forceinline__ void read_history(float (&past)[K][V], const ConvArgs
   }
 }
 
-template <int TYPE, int K, int V>
+template <int TYPE, int K, int V, bool WHOLE>
 __global__ __launch_bounds__(64 * kWaves) void conv_kernel(ConvArgs a, View<const Element<TYPE>> x, const Element<TYPE>* state,
                                                            View<Element<TYPE>> y, Element<TYPE>* state_out) {
   typedef Element<TYPE> E;
@@ -111,7 +113,7 @@ __global__ __launch_bounds__(64 * kWaves) void conv_kernel(ConvArgs a, View<cons
   Pack<E, V> in[2][kAhead];
   auto fetch = [&](Pack<E, V> (&to)[kAhead], int t) {
 #pragma unroll
-    for (int q = 0; q < kAhead; ++q) to[q] = load_channels<E, V>(x.row(min(t + q, live - 1), b), c, a.C);   // (no branch around a load)
+    for (int q = 0; q < kAhead; ++q) to[q] = load_channels<E, V, WHOLE>(x.row(min(t + q, live - 1), b), c, a.C);   // (no branch around a load)
   };
   auto work = [&](const Pack<E, V> (&from)[kAhead], int t) {
 #pragma unroll
@@ -127,7 +129,7 @@ __global__ __launch_bounds__(64 * kWaves) void conv_kernel(ConvArgs a, View<cons
 #pragma unroll
         for (int k = 0; k + 1 < K; ++k) past[k][i] = past[k + 1][i];
       }
-      if (t + q < live) store_channels<E, V>(y.row(t + q, b), c, a.C, out);
+      if (t + q < live) store_channels<E, V, WHOLE>(y.row(t + q, b), c, a.C, out);
     }
   };
   if (t0 < live) {
@@ -145,7 +147,7 @@ __global__ __launch_bounds__(64 * kWaves) void conv_kernel(ConvArgs a, View<cons
 
 // A stretch [t0, t1) owns dx there and the parameters' sums over its g; it forms g for K - 1 steps more, which dx needs.
 // The first one also owns the state's gradient, the steps -(K - 1) .. -1.
-template <int TYPE, int K, int V>
+template <int TYPE, int K, int V, bool WHOLE>
 __global__ __launch_bounds__(64 * kWaves) void conv_backward_kernel(ConvArgs a, View<const Element<TYPE>> x, const Element<TYPE>* state,
                                                                     View<const Element<TYPE>> dy, const Element<TYPE>* d_state_out,
                                                                     View<Element<TYPE>> dx, Element<TYPE>* d_state, float* partial,
@@ -178,8 +180,9 @@ __global__ __launch_bounds__(64 * kWaves) void conv_backward_kernel(ConvArgs a, 
     auto fetch = [&](int set, int t) {
 #pragma unroll
       for (int q = 0; q < kAhead; ++q) {
-        in[set][q] = load_channels<E, V>(x.row(min(t + q, last), b), c, a.C);
-        up[set][q] = load_channels<E, V>(dy.row(min(t + q, last), b), c, a.C);
+        const int at = min(t + q, max(last, t0));
+        in[set][q] = load_channels<E, V, WHOLE>(x.row(at, b), c, a.C);
+        up[set][q] = load_channels<E, V, WHOLE>(dy.row(at, b), c, a.C);
       }
     };
     auto work = [&](int set, int t) {
@@ -220,13 +223,13 @@ __global__ __launch_bounds__(64 * kWaves) void conv_backward_kernel(ConvArgs a, 
           for (int i = 0; i < V; ++i) out[i] += (float)add.v[i];
         }
         if (s >= 0) {
-          if (dx.data) store_channels<E, V>(dx.row(s, b), c, a.C, out);
+          if (dx.data) store_channels<E, V, WHOLE>(dx.row(s, b), c, a.C, out);
         } else if (d_state) {
           store_channels<E, V>(d_state + ((int64_t)(s + K - 1) * a.B + b) * a.C, c, a.C, out);
         }
       }
     };
-    const bool any = last >= t0;
+    const bool any = WHOLE || last >= t0;          // (where there is a step at all, step t0 can be read)
     if (any) fetch(0, t0);
     for (int t = t0; t < t1 + K - 1; t += 2 * kAhead) {
       if (any) fetch(1, t + kAhead);
@@ -273,7 +276,7 @@ hipError_t run_forward(const ConvArgs& a, const sprnn_conv_t* p, const sprnn_seq
   const int stretches = stretches_of(a.T, kStretch);
   const int64_t groups = (int64_t)((a.C + 64 * kWaves * V - 1) / (64 * kWaves * V)) * stretches;
   if (groups > 0x7fffffffLL) return hipErrorInvalidValue;
-  return launch(conv_kernel<TYPE, K, V>, dim3((unsigned)groups, (unsigned)a.B), dim3(64 * kWaves), 0, stream, a, view<const E>(p->x), static_cast<const E*>(p->state),
+  return launch(a.C % V == 0 ? conv_kernel<TYPE, K, V, true> : conv_kernel<TYPE, K, V, false>, dim3((unsigned)groups, (unsigned)a.B), dim3(64 * kWaves), 0, stream, a, view<const E>(p->x), static_cast<const E*>(p->state),
                 view<E>(y), static_cast<E*>(state_out));
 }
 
@@ -286,7 +289,7 @@ hipError_t run_backward(const ConvArgs& a, const sprnn_conv_t* p, const sprnn_se
   float* const partial = d_weight || d_bias ? workspace : nullptr;
   if (a.B > 0) {
     const dim3 grid((unsigned)((a.C + 64 * V - 1) / (64 * V)), (unsigned)groups, (unsigned)a.B);
-    const hipError_t e = launch(conv_backward_kernel<TYPE, K, V>, grid, dim3(64 * kWaves), 0, stream, a, view<const E>(p->x),
+    const hipError_t e = launch(a.C % V == 0 && a.T > 0 ? conv_backward_kernel<TYPE, K, V, true> : conv_backward_kernel<TYPE, K, V, false>, grid, dim3(64 * kWaves), 0, stream, a, view<const E>(p->x),
                                 static_cast<const E*>(p->state), view<const E>(dy), static_cast<const E*>(d_state_out), view<E>(dx),
                                 static_cast<E*>(d_state), partial, stretches);
     if (e != hipSuccess) return e;
