@@ -17,27 +17,30 @@
 //
 // Bound by the vector units: a state costs 13 instructions and an exponential a step, and the sums and what is done once a step
 // and channel half as much again.  8 x 1024 x 2048 with 16 states in bfloat16: 240 us, the vector units busy 80 % of them with
-// two wavefronts a SIMD (252 registers: 64 sums, 64 states and factors of a tile, 48 of the channels); the local run 65.
+// two wavefronts a SIMD (252 registers: 64 sums, 64 states and factors of a tile, 48 of the channels); the local run 58.
 #include "sprnn_scan.h"
 #include "sprnn_sums.h"
 
 namespace sprnn {
 namespace {
 
-// A segment's effect on the adjoint, from zero behind it: like the forward pass's, from the end.  One wavefront a workgroup,
-// S lanes a channel, which share out the steps of a tile; the next tile's loads are in flight while a tile is worked through.
+// A segment's effect on the adjoint, from zero behind it: like the forward pass's, from the end.  S lanes a channel share out the
+// steps of a tile; the next two tiles' loads are in flight while a tile is worked through.  The S wavefronts of a workgroup have 64
+// neighbouring channels, a row's 128 bytes, and nothing else in common: as workgroups, on several XCDs, they fetched twice
+// the bytes.
 template <int TYPE, int NS, int S>
-__global__ __launch_bounds__(64) void scan_adjoint_kernel(ScanArgs a, int segments, View<const Element<TYPE>> dys,
+__global__ __launch_bounds__(64 * S) void scan_adjoint_kernel(ScanArgs a, int segments, View<const Element<TYPE>> dys,
                                                           View<const Element<TYPE>> dts, View<const Element<TYPE>> zs,
                                                           View<const Element<TYPE>> Cs, const float* d_state_out, float* H, float* sums) {
   typedef Element<TYPE> E;
   constexpr int kRow = NS * S, kOwn = kTile * kRow / 64, kItems = kTile / S;
   static_assert(kTile * kRow % 64 == 0 && kTile % S == 0, "the tile's states and steps are dealt out evenly");
-  __shared__ __attribute__((aligned(16))) float low[2][kTile][kRow];
-  const int lane = threadIdx.x, sub = lane % S;
+  __shared__ __attribute__((aligned(16))) float every_low[S][2][kTile][kRow];
+  const int lane = threadIdx.x & 63, sub = lane % S;
+  float (&low)[2][kTile][kRow] = every_low[threadIdx.x >> 6];
   const int group = blockIdx.x / a.blocks, block = blockIdx.x - group * a.blocks;
   const int b = blockIdx.y, seg = blockIdx.z + 1, slot = segments - 1 - seg;         // nothing asks for the effect of the first one
-  const int in_group = block * (64 / S) + lane / S;
+  const int in_group = block * 64 + (int)threadIdx.x / S;
   const bool mine = in_group < a.per_group;
   const int c = group * a.per_group + min(in_group, a.per_group - 1);
   const int t0 = seg * a.segment, t1 = min(t0 + a.segment, a.T), live = min(t1, sample_end(a.lengths, b, a.T));
@@ -485,8 +488,8 @@ hipError_t run(const ScanShape& s, const sprnn_scan_t* p, const sprnn_seq_t& dy,
   hipError_t e = hipSuccess;
   if (s.B > 0) {
     if (s.back_segments > 1) {
-      a.blocks = (s.per_group + 64 / SA - 1) / (64 / SA);
-      e = launch(scan_adjoint_kernel<TYPE, NS, SA>, dim3((unsigned)(a.blocks * s.G), (unsigned)s.B, (unsigned)s.back_segments - 1), dim3(64), 0, stream, a,
+      a.blocks = (s.per_group + 63) / 64;
+      e = launch(scan_adjoint_kernel<TYPE, NS, SA>, dim3((unsigned)(a.blocks * s.G), (unsigned)s.B, (unsigned)s.back_segments - 1), dim3(64 * SA), 0, stream, a,
                  s.back_segments, io.dy, io.dt, io.z, io.C, d_state_out, workspace + w.carry, workspace + w.sums);
       if (e != hipSuccess) return e;
       carry = workspace + w.carry;
