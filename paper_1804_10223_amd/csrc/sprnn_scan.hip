@@ -324,8 +324,9 @@ int round_up(int n, int to) { return (n + to - 1) / to * to; }
 // 8 x 2048 x 4608 with 16 states has 576 wavefronts for 1024 SIMDs (850 us, with four lanes 340).  Where that is not enough time is
 // divided, which costs the local run, half of the work once more: into segments of 64 steps or more, as many as make four
 // wavefronts a SIMD (six and eight: the same within 2 %), and only where there are four at least (8 x 2048 x 4608 ragged,
-// divided in two to four: 407 us, undivided 306).  The backward pass has half as many wavefronts a channel in its main run and
-// twice the registers: two wavefronts a SIMD are all that fit, half as many segments cost less local work (441 -> 432 us).
+// divided in two to four: 407 us, undivided 306).  The backward pass's main run has one
+// wavefront for 64 channels of 16 states, and with 252 registers two of them fit a SIMD: segments that make two (a training pass of
+// 8 x 1024 x 2048 432 us) cost less local work than segments that make four (441).
 ScanShape scan_shape(const sprnn_scan_t* p) {
   ScanShape s{};
   s.T = p->steps; s.B = p->batch; s.C = p->channels; s.N = p->states; s.G = p->groups;
