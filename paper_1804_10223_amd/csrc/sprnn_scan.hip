@@ -325,8 +325,9 @@ int round_up(int n, int to) { return (n + to - 1) / to * to; }
 // divided, which costs the local run, half of the work once more: into segments of 64 steps or more, as many as make four
 // wavefronts a SIMD (six and eight: the same within 2 %), and only where there are four at least (8 x 2048 x 4608 ragged,
 // divided in two to four: 407 us, undivided 306).  The backward pass's main run has one
-// wavefront for 64 channels of 16 states, and with 252 registers two of them fit a SIMD: segments that make two (a training pass of
-// 8 x 1024 x 2048 432 us) cost less local work than segments that make four (441).
+// wavefront for 64 channels of 16 states, and with 252 registers two of them fit a SIMD: as many segments as that takes and no more
+// (512 steps, 16 states, us: 576 wavefronts a segment 367 in three, 426 in four, 626 in one; 320 198 in six, 243 in seven), and
+// two where one would leave SIMDs idle (1536: 780 in two, 830 in one).
 ScanShape scan_shape(const sprnn_scan_t* p) {
   ScanShape s{};
   s.T = p->steps; s.B = p->batch; s.C = p->channels; s.N = p->states; s.G = p->groups;
@@ -339,15 +340,16 @@ ScanShape scan_shape(const sprnn_scan_t* p) {
   s.states = 4;
   while (s.states * s.lanes < s.N) s.states *= 2;
   if (s.states * s.lanes < 8) s.states = 8;
-  auto divide = [&](int64_t waves, int* segments, int* segment) {
-    int64_t n = waves > 0 ? 4 * kSimds / waves : 1;
+  auto divide = [&](int64_t n, int least, int* segments, int* segment) {
     n = n < s.T / 64 ? n : s.T / 64;
-    if (n < 4) n = 1;
+    if (n < least) n = 1;
     *segment = round_up(s.T > 0 ? (int)((s.T + n - 1) / n) : 1, kTile);
     *segments = s.T > 0 ? (s.T + *segment - 1) / *segment : 1;
   };
-  divide(columns * s.lanes, &s.segments, &s.segment);
-  divide(2 * columns, &s.back_segments, &s.back_segment);
+  const int64_t waves = columns > 0 ? columns : kSimds;
+  divide(4 * kSimds / (waves * s.lanes), 4, &s.segments, &s.segment);
+  const int64_t pairs = 2 * kSimds / waves;
+  divide(pairs > 2 ? pairs : 2 * waves <= 3 * kSimds ? 2 : 1, 2, &s.back_segments, &s.back_segment);
   return s;
 }
 
