@@ -427,6 +427,11 @@ PROJECTS = [
     (875, 4, 144, 3601, "bf16", True, "time"),
     (1000, 4, 128, 3073, "f16", True, "time"),
     (450, 8, 368, 3400, "bf16", False, "batch"),
+    # few rows of x and more workgroups of 16 rows of w than compute units
+    (1, 24, 272, 4500, "bf16", True, "time"),
+    (3, 10, 130, 4400, "f32", True, "slice"),
+    (1, 50, 1000, 4300, "f16", False, "time"),
+    (2, 30, 256, 4200, "f32", True, "batch"),
     # 128 x 128 tiles, one to a compute unit: an even, an odd and a single number of blocks
     (20, 8, 2304, 5800, "bf16", True, "time"),
     (30, 5, 400, 8300, "f32", True, "batch"),
