@@ -5,16 +5,14 @@
 // lane's four results belong to one row of x: one scale for the four, and four neighbouring outputs.
 //
 // The instructions on e4m3 itself (v_mfma_f32_16x16x128_f8f6f4, 32 cycles a block; the older one for 32 inputs no less)
-// add the products of eight neighbours at the scale of the largest one, to about 13 bits: over random blocks the sums are
-// 1.4e-5 of their norm off, where binary32 sums are 2e-7 off.  Outputs of 16 bits, rounded by 2e-3 or 2e-4 at the end, take
-// them.  For float32 outputs the operands are widened to binary16 (exact) on their way from LDS and multiplied by
-// v_mfma_f32_16x16x32_f16, whose sums are binary32: half the rate (4 x 16 cycles), 7e-8 off.
+// add the products of eight neighbours at the scale of the largest one, to about 13 bits: a sum that cancels loses digits
+// that even an output of 16 bits has.  So the operands are widened to binary16 (exact) on their way from LDS or memory and
+// multiplied by v_mfma_f32_16x16x32_f16, whose sums are binary32, for every type of output: half the rate (4 x 16 cycles).
 #include "sprnn_seq.h"
 
 namespace sprnn {
 namespace {
 
-typedef int intx8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
@@ -93,26 +91,17 @@ __device__ __forceinline__ void store_four(E* row, int r, int rows, const floatx
   else store_part(row + r, p, rows - r);
 }
 
+__device__ __forceinline__ half8_t widen(uint32_t a, uint32_t b) {
+  const half2_t p = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)a, 1.0f, false), q = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)a, 1.0f, true);
+  const half2_t r = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)b, 1.0f, false), s = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)b, 1.0f, true);
+  return half8_t{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
+}
 // A lane's 32 inputs of one row of a block, and the product of 16 x 16 of them.
-template <bool WIDE> struct Fragment;
-template <> struct Fragment<false> {
-  intx8 v;
-  __device__ __forceinline__ Fragment(const uint4& lo, const uint4& hi)
-      : v{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w} {}
-};
-template <> struct Fragment<true> {
+struct Fragment {
   half8_t v[4];
-  static __device__ __forceinline__ half8_t widen(uint32_t a, uint32_t b) {
-    const half2_t p = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)a, 1.0f, false), q = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)a, 1.0f, true);
-    const half2_t r = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)b, 1.0f, false), s = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)b, 1.0f, true);
-    return half8_t{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
-  }
   __device__ __forceinline__ Fragment(const uint4& lo, const uint4& hi) : v{widen(lo.x, lo.y), widen(lo.z, lo.w), widen(hi.x, hi.y), widen(hi.z, hi.w)} {}
 };
-__device__ __forceinline__ floatx4 multiply(const Fragment<false>& w, const Fragment<false>& x) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.v, x.v, floatx4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0, 0, 0, 0);   // scales of one
-}
-__device__ __forceinline__ floatx4 multiply(const Fragment<true>& w, const Fragment<true>& x) {
+__device__ __forceinline__ floatx4 multiply(const Fragment& w, const Fragment& x) {
   floatx4 c = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(w.v[i], x.v[i], c, 0, 0, 0);
@@ -121,7 +110,6 @@ __device__ __forceinline__ floatx4 multiply(const Fragment<true>& w, const Fragm
 
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, Element<TYPE>* out) {
-  constexpr bool kWide = TYPE == SPRNN_TYPE_F32;
   __shared__ __attribute__((aligned(16))) uint8_t ws[2][kTileR * kSlab];
   __shared__ __attribute__((aligned(16))) uint8_t xs[2][kTileM * kSlab];
   __shared__ float scales[2][kTileM];
@@ -165,7 +153,7 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, Elemen
     for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
   const int fr = lane & 15, fq = lane >> 4;
   auto fragment = [&](const uint8_t* tile, int row) {
-    return Fragment<kWide>(*reinterpret_cast<const uint4*>(tile + piece_at(row, fq)), *reinterpret_cast<const uint4*>(tile + piece_at(row, fq + 4)));
+    return Fragment(*reinterpret_cast<const uint4*>(tile + piece_at(row, fq)), *reinterpret_cast<const uint4*>(tile + piece_at(row, fq + 4)));
   };
   fetch(0);
   for (int slab = 0; slab < a.blocks; ++slab) {
@@ -176,10 +164,10 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, Elemen
     float s[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) s[j] = scales[at][wm + j * 16 + fr];
-    const Fragment<kWide> xf[4] = {fragment(xs[at], wm + fr), fragment(xs[at], wm + 16 + fr), fragment(xs[at], wm + 32 + fr), fragment(xs[at], wm + 48 + fr)};
+    const Fragment xf[4] = {fragment(xs[at], wm + fr), fragment(xs[at], wm + 16 + fr), fragment(xs[at], wm + 32 + fr), fragment(xs[at], wm + 48 + fr)};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const Fragment<kWide> wf = fragment(ws[at], wr + i * 16 + fr);
+      const Fragment wf = fragment(ws[at], wr + i * 16 + fr);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const floatx4 block = multiply(wf, xf[j]);
@@ -208,7 +196,6 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, Elemen
 constexpr int kFewWaves = 8;
 template <int TYPE, int MT, int RT, bool WHOLE>
 __global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(ProductArgs a, Element<TYPE>* out) {
-  constexpr bool kWide = TYPE == SPRNN_TYPE_F32;
   __shared__ floatx4 sums[kFewWaves][RT * MT][64];
   const int lane = threadIdx.x & 63, fr = lane & 15, fq = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -254,11 +241,11 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(ProductArgs
   auto work = [&](const Block& f) {
 #pragma unroll
     for (int j = 0; j < MT; ++j) {
-      const Fragment<kWide> xf(f.x[j][0], f.x[j][1]);
+      const Fragment xf(f.x[j][0], f.x[j][1]);
       const float s = f.s[j] * f.ws;
 #pragma unroll
       for (int i = 0; i < RT; ++i) {
-        const floatx4 block = multiply(Fragment<kWide>(f.w[i][0], f.w[i][1]), xf);
+        const floatx4 block = multiply(Fragment(f.w[i][0], f.w[i][1]), xf);
 #pragma unroll
         for (int v = 0; v < 4; ++v) acc[i][j][v] += block[v] * s;
       }
@@ -287,68 +274,45 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(ProductArgs
   }
 }
 
-// Many rows: a wavefront multiplies 64 rows of x with 32 IR rows of w, WR x WM wavefronts are a workgroup.  Rows go from
+// Many rows: a wavefront multiplies 64 rows of x with 64 rows of w, two by two of them are a workgroup.  Rows go from
 // memory into LDS without registers between (16 bytes a lane), a slab ahead of the one that is multiplied; the swizzle of
 // piece_at is in the addresses that the lanes fetch.  Instructions of 32 x 32 take half the issue slots of 16 x 16, and the
-// vector unit needs them: with operands of 16 bits, 64 x 64 outputs of a slab are 1024 cycles of matrix instructions next to
-// 128 conversions (5 cycles) and 64 scaled sums; the widened fragments and the running sums fill the registers (IR = 4 is 27
-// too many).  On e4m3 itself the fragments are a quarter of that, and 128 x 64 outputs a wavefront halve what LDS has to
-// deliver for a matrix instruction.
+// vector unit needs them: 64 x 64 outputs of a slab are 1024 cycles of matrix instructions next to 128 conversions (5 cycles)
+// and 64 scaled sums; the widened fragments and the running sums fill the registers (128 rows of w a wavefront are 27 too many).
 // Where a CU has one workgroup, one wavefront a SIMD would go through loads from LDS, products and sums one after the other:
 // KS = 2 gives a workgroup a second set of wavefronts and stages for every other slab, and the two sums meet in the end.
-// Measured on 8192 x 2304 x 9216: float32 430 us (matrix instructions 139 us of it at 2.4 GHz; the chip runs at 2.0 here),
-// bfloat16 220.  Of the float32 form, others came out within 5 % (eight wavefronts and three stages 425, half slabs in five
-// stages 470), and widening once a workgroup, on the way into LDS, at 500: twice the bytes through LDS.
-template <int IR> struct Many;
-template <> struct Many<2> { static constexpr int kWR = 2, kWM = 2; };
-template <> struct Many<4> { static constexpr int kWR = 2, kWM = 4; };
-template <int IR> constexpr int many_r() { return Many<IR>::kWR * IR * 32; }
-template <int IR> constexpr int many_m() { return Many<IR>::kWM * 64; }
-template <int IR> constexpr int many_threads() { return Many<IR>::kWR * Many<IR>::kWM * 64; }
-template <int IR> constexpr int many_rows() { return (many_r<IR>() + many_m<IR>()) * kSlab; }          // bytes of a slab's rows
-template <int IR> constexpr int many_stage() { return many_rows<IR>() + many_threads<IR>() * 8; }       // ... and its scales
+// Measured on 8192 x 2304 x 9216: 365 us for outputs of any type (matrix instructions 139 us of it at 2.4 GHz; the chip runs at
+// 2.0 here).  Others came out within 5 % (eight wavefronts and three stages, half slabs in five stages), and widening once a
+// workgroup, on the way into LDS, a sixth slower: twice the bytes through LDS.
+constexpr int kWR = 2, kWM = 2, kIR = 2;           // wavefronts of a workgroup (and part) along w and x, 32 rows of w of each
+constexpr int kManyR = kWR * kIR * 32, kManyM = kWM * 64, kManyThreads = kWR * kWM * 64;
+constexpr int kManyRows = (kManyR + kManyM) * kSlab;                  // bytes of a slab's rows
+constexpr int kManyStage = kManyRows + kManyThreads * 8;              // ... and its scales
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 // 32 rows of a slab: this lane's four pieces, every other one of its row.
-template <bool WIDE> struct Strip;
-template <> struct Strip<false> {
-  intx8 v[2];
-  __device__ __forceinline__ void set(int i, const uint4& p) {
-    intx8& to = v[i >> 1];
-    const int at = (i & 1) * 4;
-    to[at] = (int)p.x; to[at + 1] = (int)p.y; to[at + 2] = (int)p.z; to[at + 3] = (int)p.w;
-  }
-};
-template <> struct Strip<true> {
+struct Strip {
   half8_t v[8];
   __device__ __forceinline__ void set(int i, const uint4& p) {
-    v[2 * i] = Fragment<true>::widen(p.x, p.y);
-    v[2 * i + 1] = Fragment<true>::widen(p.z, p.w);
+    v[2 * i] = widen(p.x, p.y);
+    v[2 * i + 1] = widen(p.z, p.w);
   }
 };
-__device__ __forceinline__ floatx16 multiply(const Strip<false>& w, const Strip<false>& x) {
-  floatx16 c = {};
-#pragma unroll
-  for (int i = 0; i < 2; ++i) c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w.v[i], x.v[i], c, 0, 0, 0, 0, 0, 0);
-  return c;
-}
-__device__ __forceinline__ floatx16 multiply(const Strip<true>& w, const Strip<true>& x) {
+__device__ __forceinline__ floatx16 multiply(const Strip& w, const Strip& x) {
   floatx16 c = {};
 #pragma unroll
   for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_32x32x16_f16(w.v[i], x.v[i], c, 0, 0, 0);
   return c;
 }
 
-template <int TYPE, int IR, int KS>
-__global__ __launch_bounds__(many_threads<IR>() * KS, 2) void product_many_kernel(ProductArgs a, Element<TYPE>* out) {
-  constexpr bool kWide = TYPE == SPRNN_TYPE_F32;
-  constexpr int WR = Many<IR>::kWR, kM = many_m<IR>(), kR = many_r<IR>();
-  constexpr int kWaves = many_threads<IR>() / 64, kCopiesM = kM / (kWaves * 8), kCopiesR = kR / (kWaves * 8);
+template <int TYPE, int KS>
+__global__ __launch_bounds__(kManyThreads * KS, 2) void product_many_kernel(ProductArgs a, Element<TYPE>* out) {
+  constexpr int kM = kManyM, kR = kManyR, kWaves = kManyThreads / 64, kCopiesM = kM / (kWaves * 8), kCopiesR = kR / (kWaves * 8);
   static_assert(kWaves * 8 % 16 == 0, "a lane fetches the same piece of all its rows");
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) % kWaves, part = __builtin_amdgcn_readfirstlane(tid >> 6) / kWaves;
-  uint8_t* const own_lds = lds + part * 2 * many_stage<IR>();
+  uint8_t* const own_lds = lds + part * 2 * kManyStage;
   // Workgroups go to the eight XCDs in turn: each gets a run of tiles, eight along m by a few along r at a time, whose rows
   // its L2 holds.
   const int nb = gridDim.x, bid = blockIdx.x;
@@ -375,11 +339,11 @@ __global__ __launch_bounds__(many_threads<IR>() * KS, 2) void product_many_kerne
     asm volatile("" : "+v"(from));               // one copy whatever the address, no branch
     __builtin_amdgcn_global_load_lds((Global)from, (Local)to, 16, 0, 0);
   };
-  const int wr = wave % WR * (IR * 32), wm = wave / WR * 64;
+  const int wr = wave % kWR * (kIR * 32), wm = wave / kWR * 64;
   const float* const x_scale = a.x_scales + min(m0 + wm + lane, a.vectors - 1) * a.blocks;
   const float* const w_scale = a.w_scales + (int64_t)min((r0 + wr) / 128, (a.rows - 1) / 128) * a.blocks;
   auto copy = [&](int slab, int at) {
-    uint8_t* const stage = own_lds + at * many_stage<IR>();
+    uint8_t* const stage = own_lds + at * kManyStage;
     uint8_t* const to = stage + wave * 8 * kSlab;
     const int64_t k = (int64_t)slab * kSlab;
     const bool there = k + piece < a.inputs;     // pieces are whole: the rows' length is a multiple of 16
@@ -388,7 +352,7 @@ __global__ __launch_bounds__(many_threads<IR>() * KS, 2) void product_many_kerne
 #pragma unroll
     for (int i = 0; i < kCopiesR; ++i) bring(there ? w_at[i] + k : nothing, to + (kM + i * kWaves * 8) * kSlab);
     // the scales of this wavefront's 64 rows of x, and 64 times that of its rows of w
-    uint8_t* const scales = stage + many_rows<IR>() + wave * 512;
+    uint8_t* const scales = stage + kManyRows + wave * 512;
     const int from = min(slab, a.blocks - 1);
     __builtin_amdgcn_global_load_lds((Global)(x_scale + from), (Local)scales, 4, 0, 0);
     __builtin_amdgcn_global_load_lds((Global)(w_scale + from), (Local)(scales + 256), 4, 0, 0);
@@ -403,13 +367,13 @@ __global__ __launch_bounds__(many_threads<IR>() * KS, 2) void product_many_kerne
   };
 
   const int fr = lane & 31, half = lane >> 5;
-  floatx16 acc[IR][2];
+  floatx16 acc[kIR][2];
 #pragma unroll
-  for (int i = 0; i < IR; ++i)
+  for (int i = 0; i < kIR; ++i)
 #pragma unroll
     for (int j = 0; j < 2; ++j) acc[i][j] = floatx16{};
 
-  auto strip = [&](Strip<kWide>& f, const uint8_t* tile, int row) {
+  auto strip = [&](Strip& f, const uint8_t* tile, int row) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) f.set(i, *reinterpret_cast<const uint4*>(tile + piece_at(row, 2 * i + half)));
   };
@@ -417,21 +381,21 @@ __global__ __launch_bounds__(many_threads<IR>() * KS, 2) void product_many_kerne
   next_slab();
   for (int first = 0, at = 0; first < a.blocks; first += KS, at ^= 1) {
     const int slab = first + part;
-    const uint8_t* const xs = own_lds + at * many_stage<IR>();
+    const uint8_t* const xs = own_lds + at * kManyStage;
     const uint8_t* const ws = xs + kM * kSlab;
     copy(slab + KS, at ^ 1);                     // (zeros behind the last one)
     if (KS > 1 && slab >= a.blocks) {
       next_slab();
       continue;
     }
-    const float* const scales = reinterpret_cast<const float*>(xs + many_rows<IR>() + wave * 512);
+    const float* const scales = reinterpret_cast<const float*>(xs + kManyRows + wave * 512);
     const float s[2] = {scales[fr] * scales[64], scales[32 + fr] * scales[64]};
-    Strip<kWide> xf[2];
+    Strip xf[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) strip(xf[j], xs, wm + j * 32 + fr);
 #pragma unroll
-    for (int i = 0; i < IR; ++i) {
-      Strip<kWide> wf;
+    for (int i = 0; i < kIR; ++i) {
+      Strip wf;
       strip(wf, ws, wr + i * 32 + fr);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
@@ -446,10 +410,10 @@ __global__ __launch_bounds__(many_threads<IR>() * KS, 2) void product_many_kerne
   if (KS > 1) {                                  // the parts of the slabs meet
     floatx4* const meet = reinterpret_cast<floatx4*>(lds) + wave * 64 + lane;
     constexpr int kMeet = kWaves * 64;
-    static_assert(KS == 1 || (KS == 2 && IR * 2 * 4 * kMeet * 16 + kWaves * 32 * 68 * 4 <= 4 * many_stage<IR>()), "the other part's sums and the turns fit");
+    static_assert(KS == 1 || (KS == 2 && kIR * 2 * 4 * kMeet * 16 + kWaves * 32 * 68 * 4 <= 4 * kManyStage), "the other part's sums and the turns fit");
     if (part == 1) {
 #pragma unroll
-      for (int i = 0; i < IR * 2 * 4; ++i) {
+      for (int i = 0; i < kIR * 2 * 4; ++i) {
         const floatx16& t = acc[i / 8][i / 4 % 2];
         meet[i * kMeet] = floatx4{t[4 * (i % 4)], t[4 * (i % 4) + 1], t[4 * (i % 4) + 2], t[4 * (i % 4) + 3]};
       }
@@ -457,17 +421,17 @@ __global__ __launch_bounds__(many_threads<IR>() * KS, 2) void product_many_kerne
     __syncthreads();
     if (part == 1) return;
 #pragma unroll
-    for (int i = 0; i < IR * 2 * 4; ++i) {
+    for (int i = 0; i < kIR * 2 * 4; ++i) {
       const floatx4 other = meet[i * kMeet];
 #pragma unroll
       for (int v = 0; v < 4; ++v) acc[i / 8][i / 4 % 2][4 * (i % 4) + v] += other[v];
     }
-    free_lds += IR * 2 * 4 * kMeet * 16;
+    free_lds += kIR * 2 * 4 * kMeet * 16;
   }
   // Sums leave through LDS: a lane has four neighbouring outputs of a row, 32 bytes of it a store with its neighbour.  A
   // wavefront turns its own tiles, 32 rows of x by 64 of w at a time, and stores rows of 64 outputs.
   constexpr int kPitch = 64 + 4;                 // floats; four more keep the rows of a turn off each other's banks
-  static_assert(kWaves * 32 * kPitch * 4 <= 2 * many_stage<IR>(), "a turn of every wavefront fits");
+  static_assert(kWaves * 32 * kPitch * 4 <= 2 * kManyStage, "a turn of every wavefront fits");
   float* const turn = reinterpret_cast<float*>(free_lds) + wave * 32 * kPitch;
   auto in_order = [] {                           // LDS serves a wavefront in order; the compiler is to keep it
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -475,7 +439,7 @@ __global__ __launch_bounds__(many_threads<IR>() * KS, 2) void product_many_kerne
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   };
 #pragma unroll
-  for (int pair = 0; pair < IR / 2; ++pair) {
+  for (int pair = 0; pair < kIR / 2; ++pair) {
     const int r = r0 + wr + pair * 64 + (lane & 15) * 4;
     const floatx4 bias = r < a.rows ? bias_of(a.bias, r, a.rows) : floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -506,9 +470,9 @@ template <int TYPE>
 hipError_t run_product(ProductArgs a, const sprnn_seq_t& out, hipStream_t stream) {
   Element<TYPE>* const to = static_cast<Element<TYPE>*>(out.data);
   auto groups = [&](int m, int r) { return (a.vectors + m - 1) / m * ((a.rows + r - 1) / r); };
-  // Few rows, or outputs of fewer 128 x 128 tiles than a quarter of the CUs (tiles at 128 x 2304 x 9216, 72 of them: 20 us,
-  // the few rows' kernel 26; at 768 x 5120 x 2560, 120, 40 and 78; at 256 x 5120 x 2560, 40, both 40; at 128 x 1024 x 4096, 32,
-  // 11 and 7).
+  // Few rows, or outputs of fewer 128 x 128 tiles than a quarter of the CUs (tiles at 128 x 2304 x 9216, 72 of them: 22 us,
+  // the few rows' kernel 26; at 768 x 5120 x 2560, 120, 42 and 78; at 256 x 5120 x 2560, 40, both 40; at 256 x 4096 x 1024, 16,
+  // 32 and 16).
   if (a.vectors <= 64 || groups(kTileM, kTileR) < 64) {
     const int rows = a.vectors <= 16 ? 16 : a.vectors <= 32 ? 32 : 64;
     // 16 rows of w a workgroup while each has a CU for itself, else 32 (64 rows of x, K x R: 5120 x 2560, 160 workgroups of 16, 19.0 us
@@ -523,25 +487,18 @@ hipError_t run_product(ProductArgs a, const sprnn_seq_t& out, hipStream_t stream
   }
   // Copies of 16 bytes need rows that begin and end at multiples of them.
   if (a.inputs % 16 == 0 && aligned_to(a.x, 16) && aligned_to(a.w, 16) && a.x_step % 16 == 0 && a.x_sample % 16 == 0) {
-    auto run = [&](auto kernel, int m, int r, int threads, int lds) {
-      a.tiles_m = (int)((a.vectors + m - 1) / m);
-      const int64_t n = groups(m, r);
-      if (n > 0x7fffffffLL) return hipErrorInvalidValue;
+    a.tiles_m = (int)((a.vectors + kManyM - 1) / kManyM);
+    const int64_t n = groups(kManyM, kManyR);
+    if (n > 0x7fffffffLL) return hipErrorInvalidValue;
+    auto run = [&](auto kernel, int parts) {
+      const int lds = parts * 2 * kManyStage;
       const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
       if (e != hipSuccess) return e;
-      return launch(kernel, dim3((unsigned)n), dim3((unsigned)threads), lds, stream, a, to);
+      return launch(kernel, dim3((unsigned)n), dim3((unsigned)(parts * kManyThreads)), lds, stream, a, to);
     };
-    if constexpr (TYPE != SPRNN_TYPE_F32) {
-      // Tiles of 256 x 256, one to a CU at a time, unless the last round of them leaves too many CUs idle (288 tiles at
-      // 2048 x 2304 x 9216: 82 us, 128 x 128 78).
-      const int64_t tiles = groups(many_m<4>(), many_r<4>()), rounds = (tiles + 255) / 256;
-      if (10 * tiles >= 7 * 256 * rounds)
-        return run(product_many_kernel<TYPE, 4, 1>, many_m<4>(), many_r<4>(), many_threads<4>(), 2 * many_stage<4>());
-    }
-    // One workgroup to a CU or less: two halves of the slabs side by side (256 x 2304 x 9216, 144 tiles: 20 us, one 23).
-    if (groups(many_m<2>(), many_r<2>()) <= 256)
-      return run(product_many_kernel<TYPE, 2, 2>, many_m<2>(), many_r<2>(), 2 * many_threads<2>(), 4 * many_stage<2>());
-    return run(product_many_kernel<TYPE, 2, 1>, many_m<2>(), many_r<2>(), many_threads<2>(), 2 * many_stage<2>());
+    // One workgroup to a CU or less: two halves of the slabs side by side (256 x 2304 x 9216, 144 tiles: 23 us,
+    // one 27; at 512, 288 of them, 44 and 38).
+    return n <= 256 ? run(product_many_kernel<TYPE, 2>, 2) : run(product_many_kernel<TYPE, 1>, 1);
   }
   a.tiles_m = (int)((a.vectors + kTileM - 1) / kTileM);
   const int64_t tiles = groups(kTileM, kTileR);
