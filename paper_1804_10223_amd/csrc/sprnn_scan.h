@@ -120,9 +120,11 @@ struct States {
 
 // d from v = dt + dt_bias: max(v, 0) + log1p(exp(-|v|)).  exp's argument v log2(e) and the sum 1 + e are rounded, which would
 // cost small steps (v far below 0) their last digits; what the roundings took is added to the results again (to log1p
-// undivided by 1 + e: off by less than e 2^-24).
+// undivided by 1 + e: off by less than e 2^-24).  exp(-128) is 0 in binary32, so |v| is bounded there: beyond 2.36e38 v log2(e)
+// would be infinite and the correction NaN, where a step that is masked by the type's lowest value or -infinity has d = 0.
+// (A maximum that hands NaN on: d of NaN is NaN.)
 __device__ __forceinline__ float softplus(float v) {
-  const float m = -__builtin_fabsf(v);
+  const float m = __builtin_elementwise_maximum(-__builtin_fabsf(v), -128.0f);
   const float hi = m * kLog2e, lo = __builtin_fmaf(m, kLog2e, -hi);
   float e = exp2_fast(hi);
   e = __builtin_fmaf(e, lo * kLn2, e);

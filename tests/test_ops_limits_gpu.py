@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import ops_oracle as ref
-from test_ops_gpu import BF16, F16, F32, TYPES, _close, _ops, _place
+from test_ops_gpu import BF16, F16, F32, TYPES, _close, _double, _ops, _place, _scan_case, _scan_roundings
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +50,59 @@ def test_projection_sums_are_binary32_for_every_type(T, B, K, R, type):
     want, size = ref.project(q, xs, w, ws, b), ref.project(q, xs, w, ws, b, absolute=True)
     out = ops.project_fp8(q.view(T, B, K).cuda(), xs.view(T, B, -1).cuda(), w.cuda(), ws.cuda(), b.cuda(), dtype=TYPES[type])
     _close(out, want.view(T, B, R), size.view(T, B, R), min(K, 128) + 3 + -(-K // 128) + 2, "out")
+
+
+# ---------------------------------------------------------------------------------------------------------------- scan
+
+def _masked_scan(T, B, C, N, dtype, value, seed):
+    """A scan whose every third step is masked in half of the channels by dt = value."""
+    case = _scan_case(T, B, C, N, 1, dtype, True, True, True, True, True, None, seed)
+    masked = torch.zeros((T, B, C), dtype=torch.bool)
+    masked[::3, :, ::2] = True
+    case["dt"][masked] = value
+    return case, masked
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("value", ["-inf", "lowest"])
+@pytest.mark.parametrize("T,B,C,N", [(1, 2, 70, 16), (1, 1, 9, 5), (11, 2, 70, 16), (20, 1, 33, 40), (300, 1, 24, 16), (300, 2, 10, 100)])
+def test_scan_steps_masked_by_infinity_and_the_lowest_value(T, B, C, N, value, type):
+    """d is 0 there: the state stays, the step's input does not count, and dt has no gradient."""
+    ops, dtype = _ops(), TYPES[type]
+    case, masked = _masked_scan(T, B, C, N, dtype, float("-inf") if value == "-inf" else torch.finfo(dtype).min, seed=T + C)
+    gen = torch.Generator().manual_seed(T)
+    dy, ds = torch.randn((T, B, C), generator=gen).to(dtype), torch.randn((B, C, N), generator=gen)
+    want = ref.scan(**_double(case), dy=dy.double(), d_state=ds.double())
+    size = ref.scan(**_double(case), dy=dy.double(), d_state=ds.double(), absolute=True)
+    dev = {k: v.cuda() for k, v in case.items()}
+    args = [dev[k] for k in ("u", "dt", "A", "B", "C")]
+    rest = {k: dev[k] for k in ("D", "z", "dt_bias")}
+    n = _scan_roundings(T, N, C, {**case, "dt": case["dt"][~masked]}, True)
+    for keep in (False, True):
+        y, s, *kept = ops.selective_scan(*args, state=dev["state"], keep=keep, **rest)
+        _close(y, want["y"], size["y"], n + 20, "y")
+        _close(s, want["state"], size["state"], n, "state")
+    g = ops.selective_scan_backward(dy.cuda(), *args, kept[0], d_state=ds.cuda(), **rest)
+    for name, more in (("du", 0), ("ddt", 0), ("dz", 0), ("dB", C), ("dC", C), ("dA", T * B), ("dD", T * B), ("ddt_bias", T * B), ("dstate", 0)):
+        _close(getattr(g, name), want[name], size[name], 2 * n + 60 + more, name)
+    assert (g.ddt.cpu()[masked] == 0).all()
+
+
+def test_scan_of_masked_steps_alone_leaves_the_state_and_other_ends_of_dt():
+    ops = _ops()
+    C, N = 48, 16
+    gen = torch.Generator().manual_seed(5)
+    for T in (1, 9, 400):
+        st = torch.randn((1, C, N), generator=gen).cuda()
+        u, low = torch.randn((T, 1, C), generator=gen).cuda(), torch.rand((T, 1, 1, N), generator=gen).cuda() + 0.5
+        A = -torch.rand((C, N), generator=gen).cuda() - 0.1
+        for value in (float("-inf"), torch.finfo(F32).min, -1e38, -3e38):
+            y, s = ops.selective_scan(u, torch.full_like(u, value), A, low, low, state=st)
+            assert torch.equal(s, st) and torch.isfinite(y).all()
+        # the other end: a step without end forgets the state and takes an infinite input; NaN stays NaN, in its own channel
+        dt = torch.zeros_like(u)
+        dt[T - 1, 0, 3], dt[T - 1, 0, 7] = float("inf"), float("nan")
+        y, s = ops.selective_scan(u.abs() + 0.1, dt, A, low, low, state=st)
+        assert (y[T - 1, 0, 3] == float("inf")).all() and (s[0, 3] == float("inf")).all()
+        assert torch.isnan(y[T - 1, 0, 7]) and torch.isnan(s[0, 7]).all()
+        assert int((~torch.isfinite(y)).sum()) == 2 and int((~torch.isfinite(s)).sum()) == 2 * N
