@@ -52,6 +52,10 @@ bool good_scan(const sprnn_scan_t* p);
 // there give zeros and stores to them nothing, both without a branch.  (Rows of an input may lie closer than they are long;
 // then what is read of a row that is not there is some element of another: callers do not use it.)
 constexpr int64_t kStepMost = (int64_t)1 << 25;   // elements between two steps: eight rows stay below 2^31 bytes
+// A sequence of one step may have any stride between steps: in the tiles' kernels it has the longest one, which keeps the rows
+// that are not there out of the range of the one that is.
+template <typename E>
+inline View<E> tiled_view(const sprnn_seq_t& s, int T) { return View<E>{static_cast<E*>(s.data), T > 1 ? s.step : kStepMost, s.sample}; }
 template <typename E>
 struct Tile {
   __amdgpu_buffer_rsrc_t buffer;

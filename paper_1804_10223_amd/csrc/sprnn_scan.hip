@@ -276,18 +276,20 @@ hipError_t run_prompt(ScanArgs a, const ScanShape& s, const sprnn_scan_t* p, con
                       float* kept, float* H, float* sums, hipStream_t stream) {
   typedef Element<TYPE> E;
   a.blocks = blocks_of(s);
-  const View<const E> u = view<const E>(p->u), dt = view<const E>(p->dt), z = view<const E>(p->z), B = view<const E>(p->B), C = view<const E>(p->C);
+  const View<const E> u = tiled_view<const E>(p->u, s.T), dt = tiled_view<const E>(p->dt, s.T), z = tiled_view<const E>(p->z, s.T);
+  const View<const E> B = tiled_view<const E>(p->B, s.T), C = tiled_view<const E>(p->C, s.T);
+  const View<E> to = tiled_view<E>(y, s.T);
   const dim3 block(64 * S);
   if (s.segments > 1) {
     const hipError_t e = launch(scan_kernel<TYPE, NS, S, kLocal>, dim3((unsigned)(a.blocks * s.G), (unsigned)s.B, (unsigned)s.segments - 1), block, 0, stream,
-                          a, u, dt, z, B, C, state_in, view<E>(y), (float*)nullptr, (float*)nullptr, H, sums);
+                          a, u, dt, z, B, C, state_in, to, (float*)nullptr, (float*)nullptr, H, sums);
     if (e != hipSuccess) return e;
   } else {
     H = nullptr;
     a.by_length = a.lengths && s.B > 1 && s.B <= kSamplesDealt;
   }
   return launch(kept ? scan_kernel<TYPE, NS, S, kKeeping> : scan_kernel<TYPE, NS, S, kPlain>, dim3((unsigned)(a.blocks * s.G), (unsigned)s.B, (unsigned)s.segments), block, 0, stream, a, u,
-                dt, z, B, C, state_in, view<E>(y), state_out, kept, H, sums);
+                dt, z, B, C, state_in, to, state_out, kept, H, sums);
 }
 
 template <int TYPE>

@@ -482,8 +482,9 @@ hipError_t run(const ScanShape& s, const sprnn_scan_t* p, const sprnn_seq_t& dy,
   const int64_t width = (int64_t)s.quads * s.C * 4 + 2 * (int64_t)s.C;
   ScanArgs a = scan_arguments(p, s);
   a.segment = s.back_segment;
-  BackViews<TYPE> io{view<const E>(p->u), view<const E>(p->dt), view<const E>(p->z), view<const E>(p->B), view<const E>(p->C), view<const E>(dy),
-                     view<E>(out->u), view<E>(out->dt), view<E>(out->z)};
+  auto in = [&](const sprnn_seq_t& v) { return tiled_view<const E>(v, s.T); };
+  auto to = [&](const sprnn_seq_t& v) { return tiled_view<E>(v, s.T); };
+  BackViews<TYPE> io{in(p->u), in(p->dt), in(p->z), in(p->B), in(p->C), in(dy), to(out->u), to(out->dt), to(out->z)};
   const float* carry = nullptr;
   hipError_t e = hipSuccess;
   if (s.B > 0) {

@@ -106,3 +106,55 @@ def test_scan_of_masked_steps_alone_leaves_the_state_and_other_ends_of_dt():
         assert (y[T - 1, 0, 3] == float("inf")).all() and (s[0, 3] == float("inf")).all()
         assert torch.isnan(y[T - 1, 0, 7]) and torch.isnan(s[0, 7]).all()
         assert int((~torch.isfinite(y)).sum()) == 2 and int((~torch.isfinite(s)).sum()) == 2 * N
+
+
+def _one_step(x, step):
+    """[1, B, ..] on the GPU with any stride between its steps, of which there is one."""
+    x = x.cuda()
+    return x.as_strided(x.shape, (step,) + x.stride()[1:])
+
+
+@pytest.mark.parametrize("step", [0, 1, 5, 37])
+@pytest.mark.parametrize("type", ["f32", "bf16"])
+@pytest.mark.parametrize("B,C,N", [(3, 70, 16), (2, 20, 3), (2, 130, 40)])
+def test_scan_of_one_step_whose_stride_is_shorter_than_a_row(B, C, N, type, step):
+    """The stride between steps is no part of a sequence of one step: inputs and outputs may have any, through every entry."""
+    import ctypes
+    import ops_structures as st
+    ops, dtype = _ops(), TYPES[type]
+    gen = torch.Generator().manual_seed(C)
+    case = _scan_case(1, B, C, N, 1, dtype, True, True, True, True, True, None, C)
+    dy, ds = torch.randn((1, B, C), generator=gen).to(dtype).cuda(), torch.randn((B, C, N), generator=gen).cuda()
+    dev = {k: v.cuda() for k, v in case.items()}
+    args, rest = [dev[k] for k in ("u", "dt", "A", "B", "C")], {k: dev[k] for k in ("D", "z", "dt_bias")}
+    y, s, kept = ops.selective_scan(*args, state=dev["state"], keep=True, **rest)
+    want = ops.selective_scan_backward(dy, *args, kept, d_state=ds, **rest)
+    token, _ = ops.selective_scan(*args, state=dev["state"], **rest)
+    size = ref.scan(**_double(case), absolute=True)
+    # (the token's kernel has the same roundings in another order)
+    assert ((token - y).double().cpu().abs() <= (200 * 2.0 ** -24 + 2 * ref.half_step(dtype)) * size["y"] + 2 * ref.smallest(dtype)).all()
+
+    near = {k: _one_step(case[k], step) for k in ("u", "dt", "B", "C", "z")}
+    args = [near["u"], near["dt"], dev["A"], near["B"], near["C"]]
+    rest = {"D": dev["D"], "z": near["z"], "dt_bias": dev["dt_bias"]}
+    for keep in (False, True):
+        out = torch.full((1, B, C), 7.0, dtype=dtype, device="cuda").as_strided((1, B, C), (step, C, 1))
+        got = ops.selective_scan(*args, state=dev["state"], keep=keep, out=out, **rest)
+        assert torch.equal(out, y if keep else token)
+        assert torch.equal(got[1], s) or not keep
+    again = ops.selective_scan_backward(_one_step(dy, step), *args, got[2], d_state=ds, **rest)
+    assert all(torch.equal(a, b) for a, b in zip(again, want))
+
+    # outputs of the caller's own
+    at = lambda t: st.Seq(t.data_ptr(), step, t.stride(1))
+    scan = st.Scan(1, B, C, N, 1, {F32: 0, BF16: 2}[dtype], 1, at(near["u"]), at(near["dt"]), at(near["z"]), at(near["B"]), at(near["C"]),
+                   dev["A"].data_ptr(), dev["D"].data_ptr(), dev["dt_bias"].data_ptr(), None)
+    own = {k: torch.full_like(getattr(want, k), 7.0) for k in ("du", "ddt", "dz", "dB", "dC")}
+    g = st.ScanGradientBuffers(*[at(own[k]) for k in ("du", "ddt", "dz", "dB", "dC")], None, None, None, None)
+    need = ops.scan_sizes(1, B, C, N, 1)[1]
+    work = torch.empty(need, dtype=torch.uint8, device="cuda")
+    assert ops._library().sprnn_scan_backward(0, ctypes.byref(scan), ops.Seq(dy.data_ptr(), step, C), ds.data_ptr(), kept.data_ptr(),
+                                              ctypes.byref(g), work.data_ptr(), need, torch.cuda.current_stream().cuda_stream) == 0
+    torch.cuda.synchronize()
+    for name, got in own.items():
+        assert torch.equal(got, getattr(want, name)), name
