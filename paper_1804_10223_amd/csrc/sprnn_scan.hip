@@ -367,15 +367,17 @@ static void scan_sizes(const ScanShape& s, int64_t* forward, int64_t* backward, 
   *backward = scan_backward_bytes(s);
 }
 
-static bool good_rows(const sprnn_seq_t& s, int type) { return good_view(s, type) && s.step <= kStepMost; }
-static bool good_rows(const sprnn_seq_t& s, int type, int T, int B, int width) { return good_output(s, type, T, B, width) && s.step <= kStepMost; }
+// (the stride between steps is limited where there are two)
+static bool good_step(const sprnn_seq_t& s, int T) { return T <= 1 || s.step <= kStepMost; }
+static bool good_rows(const sprnn_seq_t& s, int type, int T) { return good_view(s, type) && good_step(s, T); }
+static bool good_rows(const sprnn_seq_t& s, int type, int T, int B, int width) { return good_output(s, type, T, B, width) && good_step(s, T); }
 
 static bool good_arguments(const sprnn_scan_t* p) {
   if (!good_scan(p) || !activation_type(p->type) || (p->softplus != 0 && p->softplus != 1)) return false;
   if (!p->A || !aligned_to(p->A, 4) || !aligned_to(p->D, 4) || !aligned_to(p->dt_bias, 4) || !aligned_to(p->lengths, 4)) return false;
   if (p->steps == 0 || p->batch == 0) return true;
-  const int type = p->type;
-  return good_rows(p->u, type) && good_rows(p->dt, type) && (!p->z.data || good_rows(p->z, type)) && good_rows(p->B, type) && good_rows(p->C, type);
+  auto good = [&](const sprnn_seq_t& s) { return good_rows(s, p->type, p->steps); };
+  return good(p->u) && good(p->dt) && (!p->z.data || good(p->z)) && good(p->B) && good(p->C);
 }
 
 }  // namespace sprnn
@@ -425,7 +427,7 @@ int sprnn_scan_backward(int device_id, const sprnn_scan_t* scan, sprnn_seq_t dy,
     return SPRNN_ERR_INVALID;
   if (s.T > 0 && s.B > 0) {
     auto good = [&](const sprnn_seq_t& o, int width) { return !o.data || good_rows(o, scan->type, s.T, s.B, width); };
-    if (!kept || !good_rows(dy, scan->type) || !good(g.u, s.C) || !good(g.dt, s.C) || !good(g.z, s.C) || !good(g.B, s.G * s.N) || !good(g.C, s.G * s.N))
+    if (!kept || !good_rows(dy, scan->type, s.T) || !good(g.u, s.C) || !good(g.dt, s.C) || !good(g.z, s.C) || !good(g.B, s.G * s.N) || !good(g.C, s.G * s.N))
       return SPRNN_ERR_INVALID;
     if (g.z.data && !scan->z.data) return SPRNN_ERR_INVALID;
   }

@@ -114,10 +114,10 @@ def _one_step(x, step):
     return x.as_strided(x.shape, (step,) + x.stride()[1:])
 
 
-@pytest.mark.parametrize("step", [0, 1, 5, 37])
+@pytest.mark.parametrize("step", [0, 1, 5, 37, (1 << 25) + 1, 1 << 31, (1 << 33) - 4])
 @pytest.mark.parametrize("type", ["f32", "bf16"])
 @pytest.mark.parametrize("B,C,N", [(3, 70, 16), (2, 20, 3), (2, 130, 40)])
-def test_scan_of_one_step_whose_stride_is_shorter_than_a_row(B, C, N, type, step):
+def test_scan_of_one_step_with_any_stride_between_steps(B, C, N, type, step):
     """The stride between steps is no part of a sequence of one step: inputs and outputs may have any, through every entry."""
     import ctypes
     import ops_structures as st
