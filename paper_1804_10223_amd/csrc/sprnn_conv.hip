@@ -286,7 +286,8 @@ hipError_t run_backward(const ConvArgs& a, const sprnn_conv_t* p, const sprnn_se
   typedef Element<TYPE> E;
   constexpr int V = 2;                           // the window of g and the parameters' sums are in registers, too
   const int stretches = stretches_of(a.T, kStretchBack), groups = groups_of(stretches);
-  float* const partial = d_weight || d_bias ? workspace : nullptr;
+  const bool summed = d_weight || d_bias;
+  float* const partial = summed ? workspace : nullptr;         // (none without a sample: sums of nothing are zeros)
   if (a.B > 0) {
     const dim3 grid((unsigned)((a.C + 64 * V - 1) / (64 * V)), (unsigned)groups, (unsigned)a.B);
     const hipError_t e = launch(a.C % V == 0 && a.T > 0 ? conv_backward_kernel<TYPE, K, V, true> : conv_backward_kernel<TYPE, K, V, false>, grid, dim3(64 * kWaves), 0, stream, a, view<const E>(p->x),
@@ -294,7 +295,7 @@ hipError_t run_backward(const ConvArgs& a, const sprnn_conv_t* p, const sprnn_se
                                 static_cast<E*>(d_state), partial, stretches);
     if (e != hipSuccess) return e;
   }
-  if (!partial) return hipSuccess;
+  if (!summed) return hipSuccess;
   return launch_sum_partials(partial, groups * a.B, (int64_t)(K + 1) * a.C, PutParameters{d_weight, d_bias, a.C, K}, stream);
 }
 

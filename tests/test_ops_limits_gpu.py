@@ -158,3 +158,23 @@ def test_scan_of_one_step_with_any_stride_between_steps(B, C, N, type, step):
     torch.cuda.synchronize()
     for name, got in own.items():
         assert torch.equal(got, getattr(want, name)), name
+
+
+# ---------------------------------------------------------------------------------------------------------------- conv
+
+@pytest.mark.parametrize("T", [0, 5])
+def test_conv_gradients_without_a_sample_are_zeros(T):
+    import ctypes
+    import ops_structures as st
+    ops = _ops()
+    C, K = 70, 4
+    weight, bias = torch.ones((C, K), device="cuda"), torch.ones(C, device="cuda")
+    conv = st.Conv(T, 0, C, K, 0, 1, st.Seq(None, C, C), weight.data_ptr(), bias.data_ptr(), None, None)
+    dw, db = torch.full((C, K), 7.0, device="cuda"), torch.full((C,), 7.0, device="cuda")
+    assert ops._library().sprnn_conv_backward(0, ctypes.byref(conv), ops.Seq(), None, ops.Seq(), dw.data_ptr(), db.data_ptr(), None, None, 0,
+                                              torch.cuda.current_stream().cuda_stream) == 0
+    torch.cuda.synchronize()
+    assert (dw == 0).all() and (db == 0).all()
+    x = torch.zeros((T, 0, C), device="cuda")
+    dx, dw, db, ds = ops.causal_conv_backward(x, x, weight, bias)
+    assert dx.shape == x.shape and ds.shape == (K - 1, 0, C) and (dw == 0).all() and (db == 0).all()
