@@ -410,22 +410,24 @@ __global__ __launch_bounds__(64 * waves_of(S), 2) void scan_backward_kernel(Scan
   }
 }
 
-// dB and dC from the sums of the blocks of channels: one lane per (step, sample, group, dB or dC, state).
+// dB and dC from the sums of the blocks of channels: one lane per (step, sample, group, dB or dC, state) at a time (a launch has
+// fewer than 2^32 lanes).
+constexpr int64_t kLowGroups = 1 << 20;
 template <int TYPE>
 __global__ __launch_bounds__(256) void scan_low_gradients_kernel(ScanArgs a, int row, const float* partial, View<Element<TYPE>> dB,
                                                                  View<Element<TYPE>> dC) {
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, width = (int64_t)a.G * 2 * row;
-  const int64_t all = (int64_t)a.T * a.B * width;
-  if (at >= all) return;
-  const int n = (int)(at % row), which = (int)(at / row % 2), group = (int)(at / (2 * row) % a.G);
-  const int64_t vector = at / width;
-  const int t = (int)(vector / a.B), b = (int)(vector % a.B);
-  const View<Element<TYPE>> out = which ? dC : dB;
-  if (n >= a.N || !out.data) return;
-  float sum = 0.0f;
-  if (t < sample_end(a.lengths, b, a.T))
-    for (int k = 0; k < a.blocks; ++k) sum += partial[k * all + at];
-  out.row(t, b)[(int64_t)group * a.N + n] = (Element<TYPE>)sum;
+  const int64_t width = (int64_t)a.G * 2 * row, all = (int64_t)a.T * a.B * width;
+  for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < all; at += (int64_t)gridDim.x * 256) {
+    const int n = (int)(at % row), which = (int)(at / row % 2), group = (int)(at / (2 * row) % a.G);
+    const int64_t vector = at / width;
+    const int t = (int)(vector / a.B), b = (int)(vector % a.B);
+    const View<Element<TYPE>> out = which ? dC : dB;
+    if (n >= a.N || !out.data) continue;
+    float sum = 0.0f;
+    if (t < sample_end(a.lengths, b, a.T))
+      for (int k = 0; k < a.blocks; ++k) sum += partial[k * all + at];
+    out.row(t, b)[(int64_t)group * a.N + n] = (Element<TYPE>)sum;
+  }
 }
 
 // Sums [quads][C][4], [C], [C] to dA [C][N], dD and d dt_bias [C].
@@ -501,7 +503,7 @@ hipError_t run(const ScanShape& s, const sprnn_scan_t* p, const sprnn_seq_t& dy,
     if (e != hipSuccess) return e;
     const int64_t lows = (int64_t)s.T * s.B * s.G * 8 * S;
     if (lows > 0 && (out->B.data || out->C.data)) {
-      e = launch(scan_low_gradients_kernel<TYPE>, dim3((unsigned)((lows + 255) / 256)), dim3(256), 0, stream, a, 4 * S,
+      e = launch(scan_low_gradients_kernel<TYPE>, dim3((unsigned)(lows < 256 * kLowGroups ? (lows + 255) / 256 : kLowGroups)), dim3(256), 0, stream, a, 4 * S,
                  (const float*)(workspace + w.partial), view<E>(out->B), view<E>(out->C));
       if (e != hipSuccess) return e;
     }

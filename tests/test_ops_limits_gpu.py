@@ -178,3 +178,42 @@ def test_conv_gradients_without_a_sample_are_zeros(T):
     x = torch.zeros((T, 0, C), device="cuda")
     dx, dw, db, ds = ops.causal_conv_backward(x, x, weight, bias)
     assert dx.shape == x.shape and ds.shape == (K - 1, 0, C) and (dw == 0).all() and (db == 0).all()
+
+
+def test_scan_gradients_of_more_sums_than_a_launch_has_lanes():
+    """A group for every channel: 2^32 sums of dB and dC.  Each group is a scan of its own, so a few of them make the reference."""
+    import ctypes
+    import ops_structures as st
+    ops = _ops()
+    T, B, C, some = 64, 8, 1 << 20, 64
+    gen = torch.Generator().manual_seed(1)
+    one = {k: torch.randn(C, generator=gen).to(BF16).cuda() for k in ("u", "dt", "B", "C", "dy")}
+    A = -torch.rand((C, 1), generator=gen).cuda() - 0.05
+    ends = torch.tensor([64, 1, 33, 64, 0, 7, 64, 64], dtype=torch.int32, device="cuda")
+
+    def backward(part):
+        n = A[part].shape[0]
+        rows = {k: v[part].expand(T, B, n) for k, v in one.items()}            # every step and sample has the same inputs
+        low = {k: rows[k].unsqueeze(-1) for k in ("B", "C")}
+        _, _, kept = ops.selective_scan(rows["u"], rows["dt"], A[part], low["B"], low["C"], lengths=ends, keep=True)
+        at = lambda t: st.Seq(t.data_ptr(), t.stride(0), t.stride(1))
+        scan = st.Scan(T, B, n, 1, n, 2, 1, at(rows["u"]), at(rows["dt"]), st.Seq(), at(rows["B"]), at(rows["C"]), A[part].data_ptr(), None, None,
+                       ends.data_ptr())
+        dB, dC = (torch.full((T, B, n), 7.0, dtype=BF16, device="cuda") for _ in range(2))
+        g = st.ScanGradientBuffers(B=at(dB), C=at(dC))
+        need = ops.scan_sizes(T, B, n, 1, n)[1]
+        work = torch.empty(need, dtype=torch.uint8, device="cuda")
+        dy = rows["dy"]
+        assert ops._library().sprnn_scan_backward(0, ctypes.byref(scan), ops.Seq(dy.data_ptr(), dy.stride(0), dy.stride(1)), None, kept.data_ptr(),
+                                                  ctypes.byref(g), work.data_ptr(), need, torch.cuda.current_stream().cuda_stream) == 0
+        torch.cuda.synchronize()
+        return dB, dC
+
+    whole = backward(slice(0, C))
+    for first in (0, C // 2 - 5, C - some):
+        part = slice(first, first + some)
+        for got, want in zip(whole, backward(part)):
+            assert torch.equal(got[:, :, part], want) and torch.isfinite(want).all() and float(want.abs().max()) > 0
+            for b, n in enumerate(ends.tolist()):
+                assert (want[n:, b] == 0).all()
+    assert not (whole[0] == 7.0).all(dim=2).any()
