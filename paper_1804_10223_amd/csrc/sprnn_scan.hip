@@ -323,13 +323,16 @@ int round_up(int n, int to) { return (n + to - 1) / to * to; }
 
 // How many lanes share a channel: as few as its states need (16 a lane at most), and more, down to four states a lane, while
 // there are fewer wavefronts than twice the SIMDs: sharing costs a tenth more instructions, but with one lane a channel
-// 8 x 2048 x 4608 with 16 states has 576 wavefronts for 1024 SIMDs (850 us, with four lanes 340).  Where that is not enough time is
+// 8 x 2048 x 4608 with 16 states has 576 wavefronts for 1024 SIMDs (540 us, with four lanes 461).  Where that is not enough time is
 // divided, which costs the local run, half of the work once more: into segments of 64 steps or more, as many as make four
-// wavefronts a SIMD (six and eight: the same within 2 %), and only where there are four at least (8 x 2048 x 4608 ragged,
-// divided in two to four: 407 us, undivided 306).  The backward pass's main run has one
+// wavefronts a SIMD (six and eight: the same within 3 %, or up to a fifth longer), and only where there are four at least
+// (8 x 2048 x 4608, divided in two to four: 537 to 520 us; ragged 422 to 383, undivided 290).  The backward pass's main run has one
 // wavefront for 64 channels of 16 states, and with 252 registers two of them fit a SIMD: as many segments as that takes and no more
-// (512 steps, 16 states, us: 576 wavefronts a segment 367 in three, 426 in four, 626 in one; 320 198 in six, 243 in seven), and
-// two where one would leave SIMDs idle (1536: 780 in two, 830 in one).
+// (512 steps, 16 states, us: 576 wavefronts a segment 366 in three, 468 in two, 633 in one; 320 199 in six, 255 in three), and
+// two where one would leave SIMDs idle (1536: 788 in two, 834 in one, 846 in three).  With more states a wavefront has 16 or 8
+// channels, but LDS leaves a CU one or two workgroups, so that the count of 64 channels serves there as well (512 steps, 8 samples, us:
+// 2304 channels of 32 states 364 in seven, 351 in five, 374 in three, 438 in one; 1152 of 128 states 871 in eight, 838 in five, 1126 in one;
+// 1152 of 64 states 372 in eight, 319 in seven, 728 in one).
 ScanShape scan_shape(const sprnn_scan_t* p) {
   ScanShape s{};
   s.T = p->steps; s.B = p->batch; s.C = p->channels; s.N = p->states; s.G = p->groups;
