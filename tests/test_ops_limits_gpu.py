@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import ops_oracle as ref
+import ops_slow_decay as slow
 from test_ops_gpu import BF16, F16, F32, TYPES, _close, _double, _ops, _place, _scan_case, _scan_roundings
 
 pytestmark = pytest.mark.gpu
@@ -217,3 +218,24 @@ def test_scan_gradients_of_more_sums_than_a_launch_has_lanes():
             for b, n in enumerate(ends.tolist()):
                 assert (want[n:, b] == 0).all()
     assert not (whole[0] == 7.0).all(dim=2).any()
+
+
+@pytest.mark.parametrize("T,B,C,N,G,dtype,lengths", slow.CASES)
+def test_scans_that_forget_slowly_hold_their_state_in_binary32(T, B, C, N, G, dtype, lengths):
+    """Over all elements, not in the worst case: a state that is rounded to 16 bits anywhere along the way is far outside."""
+    ops = _ops()
+    case, dy, ds = slow.make(T, B, C, N, G, dtype, T)
+    want = ref.scan(**_double(case), lengths=lengths, dy=dy.double(), d_state=ds.double())
+    dev = {k: v.cuda() for k, v in case.items()}
+    args, rest = [dev[k] for k in ("u", "dt", "A", "B", "C")], {k: dev[k] for k in ("D", "z", "dt_bias")}
+    rest["lengths"] = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    y, s = ops.selective_scan(*args, state=dev["state"], **rest)
+    y2, s2, kept = ops.selective_scan(*args, state=dev["state"], keep=True, **rest)
+    assert torch.equal(y, y2) and torch.equal(s, s2)
+    off = {"y": slow.distance(y, want["y"]) / slow.allowed(case, False, dtype), "state": slow.distance(s, want["state"]) / slow.allowed(case)}
+    g = ops.selective_scan_backward(dy.cuda(), *args, kept, d_state=ds.cuda(), **rest)
+    for name in g._fields:
+        got = getattr(g, name)
+        off[name] = slow.distance(got, want[name]) / slow.allowed(case, True, got.dtype)
+    print("of the bound: " + ", ".join("%s %.3f" % x for x in off.items()), flush=True)
+    assert max(off.values()) <= 1.0, off
