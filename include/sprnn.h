@@ -450,6 +450,9 @@ typedef struct sprnn_seq_s {
  *   y_t[c] = (sum_n C_t[g][n] h_t[c][n] + D[c] u_t[c]) * silu(z_t[c])
  * d_t A is expected to be at most 0 (A negative, d_t positive), as such layers are.  C is at most 2^20 here, and two steps
  * of a sequence are at most 2^25 elements apart.
+ * A step with dt = -infinity (or the type's lowest value) is masked with softplus = 1: d_t is 0, the state stays, dt_t has no
+ * gradient.  From a step on whose d_t u_t is infinite or NaN, its channel's y and state, and the gradients that meet it, are
+ * infinite or NaN, not always which of the two the formula says (states that fill up a lane are zeros that it is multiplied with).
  */
 typedef struct sprnn_scan_s {
   int steps, batch;            /* T, B                                                                  */
@@ -580,7 +583,8 @@ int sprnn_rms_norm_backward(int device_id, const sprnn_norm_t* norm, sprnn_seq_t
  *   bias            float32 [R] or NULL.
  *   out             [T][B][R] of out_type (SPRNN_TYPE_F32, F16, BF16).  float32 and contiguous it is the x of the forward
  *                   calls above.
- * The gradient of x is the same call with the gradient of out in 8 bits and w transposed.
+ * The gradient of x is the same call with the gradient of out in 8 bits, a scale per 128, and w and w_scales transposed; both are
+ * the caller's to make (nothing here quantises a gradient or a weight, or forms the gradient of w).
  */
 typedef struct sprnn_product_s {
   int steps, batch, rows, inputs;
