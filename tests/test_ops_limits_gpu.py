@@ -239,3 +239,83 @@ def test_scans_that_forget_slowly_hold_their_state_in_binary32(T, B, C, N, G, dt
         off[name] = slow.distance(got, want[name]) / slow.allowed(case, True, got.dtype)
     print("of the bound: " + ", ".join("%s %.3f" % x for x in off.items()), flush=True)
     assert max(off.values()) <= 1.0, off
+
+
+@pytest.mark.parametrize("T", [9, 300])
+def test_what_lies_behind_a_samples_end_is_neither_used_nor_changed(T):
+    """Every operator with lengths: the same bits whatever stands behind the ends, zeros in the outputs there, inputs untouched."""
+    ops = _ops()
+    B, C, N, K = 4, 70, 16, 4
+    ends = [T, T // 2 + 1, 1, 0]
+    lengths = torch.tensor(ends, dtype=torch.int32, device="cuda")
+    gen = torch.Generator().manual_seed(T)
+    inputs = {k: torch.randn((T, B, C), generator=gen).to(BF16) for k in ("u", "dt", "z", "dy")}
+    inputs.update({k: torch.randn((T, B, 1, N), generator=gen).to(BF16) for k in ("B", "C")})
+    A, weight = -torch.rand((C, N), generator=gen).cuda() - 0.1, torch.randn((C, K), generator=gen).cuda()
+    runs = []
+    for fill in (0.0, float("nan"), float("inf"), torch.finfo(BF16).min):
+        own = {k: v.clone() for k, v in inputs.items()}
+        for v in own.values():
+            for b, n in enumerate(ends):
+                v[n:, b] = fill
+        dev = {k: v.cuda() for k, v in own.items()}
+        y, s, kept = ops.selective_scan(dev["u"], dev["dt"], A, dev["B"], dev["C"], z=dev["z"], lengths=lengths, keep=True)
+        g = ops.selective_scan_backward(dev["dy"], dev["u"], dev["dt"], A, dev["B"], dev["C"], kept, z=dev["z"], lengths=lengths)
+        c, cs = ops.causal_conv(dev["u"], weight, lengths=lengths)
+        dx, dw, _, dcs = ops.causal_conv_backward(dev["dy"], dev["u"], weight, lengths=lengths)
+        for b, n in enumerate(ends):
+            for out in (y, g.du, g.ddt, g.dz, g.dB, g.dC, c, dx):
+                assert (out[n:, b] == 0).all()
+        bits = lambda t: t.cpu().view(torch.int16)
+        assert all(torch.equal(bits(dev[k]), own[k].view(torch.int16)) for k in own)
+        runs.append((y, s, g.du, g.ddt, g.dA, g.dB, g.dC, g.dz, g.dstate, c, cs, dx, dw, dcs))
+    for run in runs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(run, runs[0]))
+
+
+# T, B, K, R: few rows, tiles with two halves of the slabs, tiles with one, rows without whole pieces
+@pytest.mark.parametrize("T,B,K,R", [(1, 8, 256, 300), (20, 8, 640, 5800), (64, 32, 384, 2560), (20, 8, 130, 5800)])
+def test_captured_projections_replay_like_eager_ones(T, B, K, R):
+    """Every kernel of the projection in a graph, on new inputs and between eager calls."""
+    ops = _ops()
+    gen = torch.Generator().manual_seed(K)
+    e4m3 = lambda *s: torch.randn(s, generator=gen).to(torch.float8_e4m3fn)
+    x, w = e4m3(T, B, K).cuda(), e4m3(R, K).cuda()
+    xs, ws = torch.rand((T, B, -(-K // 128)), generator=gen).cuda(), torch.rand((-(-R // 128), -(-K // 128)), generator=gen).cuda()
+    call = lambda: [ops.project_fp8(x, xs, w, ws, dtype=t) for t in (F32, F16, BF16)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            outputs = call()
+    torch.cuda.current_stream().wait_stream(side)
+    for turn in range(4):
+        x.copy_(e4m3(T, B, K))
+        xs.copy_(torch.rand(xs.shape, generator=gen))
+        want = call()
+        for o in outputs:
+            o.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outputs, want)), turn
+        assert all(torch.isfinite(o.float()).all() for o in (outputs[0], outputs[2]))
+
+
+def test_the_gradient_of_x_is_the_projection_with_the_weights_transposed():
+    """dx = d out w: the gradient of out brought to 8 bits by the caller, w and its scales transposed."""
+    ops = _ops()
+    T, B, K, R = 7, 9, 272, 400
+    gen = torch.Generator().manual_seed(2)
+    normal = lambda *s: torch.randn(s, generator=gen, dtype=torch.float64)
+    w, ws = ref.blocks(normal(R, K) / K ** 0.5, 128, 128)
+    d, ds = ref.blocks(normal(T * B, R), 1, 128)
+    wt, wst = w.view(torch.uint8).t().contiguous().view(torch.float8_e4m3fn), ws.t().contiguous()
+    dx = ops.project_fp8(d.view(T, B, R).cuda(), ds.view(T, B, -1).cuda(), wt.cuda(), wst.cuda())
+    # what autograd gives for the dequantised product
+    x = normal(T * B, K).requires_grad_()
+    full = w.double() * ws.double().repeat_interleave(128, 0)[:R].repeat_interleave(128, 1)[:, :K]
+    grad = d.double() * ds.double().repeat_interleave(128, 1)[:, :R]
+    (want,) = torch.autograd.grad((x @ full.t() * grad).sum(), [x])
+    _close(dx, want.view(T, B, K), ref.project(d, ds, wt, wst, absolute=True).view(T, B, K), 128 + 3 + -(-R // 128) + 2, "dx")
