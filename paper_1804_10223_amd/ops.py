@@ -6,13 +6,15 @@ or bfloat16 CUDA tensors whose last dimension is contiguous (the first two may h
 range of the channels of a wider tensor need no copy); parameters and states are contiguous float32 tensors.  Outputs
 that the caller does not pass are allocated here, contiguous.  ``lengths`` (int32 [B], on the device) ends samples early:
 inputs behind a sample's end are not used, outputs there are zero.  Nothing here takes part in autograd: the backward
-passes are calls of their own, like those of ``SparseRNN``.
+passes are calls of their own, like those of ``SparseRNN``, and a call on tensors that require gradients warns that its
+results have none (not under ``torch.no_grad``).
 """
 from __future__ import annotations
 
 import ctypes
 import functools
 import struct
+import warnings
 from typing import NamedTuple, Optional
 
 import torch
@@ -140,6 +142,15 @@ def _workspace(size, device):
     return torch.empty((size,), dtype=torch.uint8, device=device) if size else None
 
 
+def _leads(t):
+    return t is not None and t.requires_grad
+
+
+def _warn(what, level=3):
+    warnings.warn("%s: an argument requires gradients, the results have no graph (the gradients are a call of their own; use "
+                  "torch.no_grad or detach where none are wanted)" % what, stacklevel=level)
+
+
 def _at(t):
     return 0 if t is None else t.data_ptr()
 
@@ -186,6 +197,10 @@ def selective_scan(u, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=True, 
     state_out may be state itself (the next token of running sequences: T = 1 with the state in place)."""
     index = _index(u, "u")
     scan, T, batch, channels, states, groups = _scan(index, u, dt, A, B, C, D, z, dt_bias, softplus, lengths)
+    if torch.is_grad_enabled() and (
+            u.requires_grad or dt.requires_grad or A.requires_grad or B.requires_grad or C.requires_grad or _leads(D) or _leads(z) or
+            _leads(dt_bias) or _leads(state)):
+        _warn("selective_scan")
     dtype, device, full = u.dtype, u.device, (batch, channels, states)
     if out is None:
         out = torch.empty((T, batch, channels), dtype=dtype, device=device)
@@ -246,6 +261,8 @@ def causal_conv(x, weight, bias=None, silu=True, state=None, lengths=None, out=N
     -> (y [T, B, C], the last K - 1 inputs [K - 1, B, C]).  state_out may be state itself."""
     index = _index(x, "x")
     conv, T, batch, channels, width = _conv(index, x, weight, bias, silu, state, lengths)
+    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or _leads(bias) or _leads(state)):
+        _warn("causal_conv")
     dtype, wide, past = x.dtype, (T, batch, channels), (max(width - 1, 0), batch, channels)
     if out is None:
         out = torch.empty(wide, dtype=dtype, device=x.device)
@@ -291,6 +308,8 @@ def _norm_forward(x, weight, eps, residual, residual_out, y, scales, quantized):
     shape, dtype, device = x.shape, x.dtype, x.device
     stream_dtype = dtype if residual is None else residual.dtype
     norm = _norm(index, shape, dtype, stream_dtype, eps, weight)
+    if torch.is_grad_enabled() and (x.requires_grad or _leads(weight) or _leads(residual)):
+        _warn("rms_norm_fp8" if quantized else "rms_norm", 4)
     y_dtype, blocks = E4M3 if quantized else dtype, (shape[0], shape[1], (shape[2] + 127) // 128)
     if residual_out is None and residual is not None:
         residual_out = torch.empty(shape, dtype=stream_dtype, device=device)
@@ -358,6 +377,8 @@ def project_fp8(x, x_scales, w, w_scales, bias=None, dtype=None, out=None):
     product = _PRODUCT.pack(T, batch, rows, inputs, *_seq(x, shape, E4M3, index, "x"), _plain(x_scales, (T, batch, blocks), F32, index, "x_scales"),
                             _plain(w, (rows, inputs), E4M3, index, "w"),
                             _plain(w_scales, ((rows + 127) // 128, blocks), F32, index, "w_scales"), _plain(bias, (rows,), F32, index, "bias"))
+    if torch.is_grad_enabled() and (x.requires_grad or x_scales.requires_grad or w.requires_grad or w_scales.requires_grad or _leads(bias)):
+        _warn("project_fp8")
     if out is None:
         out = torch.empty((T, batch, rows), dtype=F32 if dtype is None else dtype, device=x.device)
     elif dtype is not None and out.dtype != dtype:

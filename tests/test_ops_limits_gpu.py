@@ -319,3 +319,29 @@ def test_the_gradient_of_x_is_the_projection_with_the_weights_transposed():
     grad = d.double() * ds.double().repeat_interleave(128, 1)[:, :R]
     (want,) = torch.autograd.grad((x @ full.t() * grad).sum(), [x])
     _close(dx, want.view(T, B, K), ref.project(d, ds, wt, wst, absolute=True).view(T, B, K), 128 + 3 + -(-R // 128) + 2, "dx")
+
+
+def test_calls_on_tensors_that_require_gradients_say_that_there_are_none():
+    import warnings
+    ops = _ops()
+    x, A = torch.zeros((2, 1, 8), device="cuda"), torch.zeros((8, 4), device="cuda")
+    low, one = torch.zeros((2, 1, 1, 4), device="cuda"), torch.ones((2, 1, 1), device="cuda")
+    q, eight = torch.zeros((2, 1, 8), dtype=torch.float8_e4m3fn, device="cuda"), torch.zeros(8, device="cuda")
+    leaf = lambda t: t.clone().requires_grad_()
+    calls = [lambda: ops.selective_scan(leaf(x), x, A, low, low), lambda: ops.selective_scan(x, x, leaf(A), low, low),
+             lambda: ops.selective_scan(x, x, A, low, low, D=leaf(eight)), lambda: ops.causal_conv(x, leaf(A)),
+             lambda: ops.causal_conv(x, A, bias=leaf(eight)), lambda: ops.rms_norm(leaf(x)), lambda: ops.rms_norm(x, leaf(eight)),
+             lambda: ops.rms_norm_fp8(x, residual=leaf(x)), lambda: ops.project_fp8(q, one, q[:, 0], one[0], bias=leaf(eight[:2]))]
+    for call in calls:
+        with pytest.warns(UserWarning, match="have no graph") as said:
+            call()
+        assert len(said) == 1 and said[0].filename == __file__
+        with torch.no_grad(), warnings.catch_warnings():
+            warnings.simplefilter("error")
+            call()
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        ops.selective_scan(leaf(x).detach(), x, A, low, low)
+        ops.causal_conv(x, A)
+        ops.rms_norm(x, eight)
+        ops.project_fp8(q, one, q[:, 0], one[0])
