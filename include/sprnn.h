@@ -576,7 +576,8 @@ int sprnn_rms_norm_backward(int device_id, const sprnn_norm_t* norm, sprnn_seq_t
  * The input projection of sprnn_project with operands of 8 bits: rows of x in e4m3 with a scale per 128 (as sprnn_rms_norm
  * writes them), weights in e4m3 with a scale per 128 x 128,
  *   out[t][b][r] = sum_k (x[t][b][k] sx[t][b][k / 128]) (w[r][k] sw[r / 128][k / 128]) + bias[r].
- * Products are exact and all sums are float32, for every type of out.
+ * Products are exact and all sums are float32, for every type of out.  sx sw is formed first, in float32: where it leaves the
+ * normal range (1.2e-38 to 3.4e38), results lose digits or are not finite.
  *   steps, batch    T, B;  rows: R, outputs of a vector;  inputs: K.
  *   x               e4m3 [T][B][K];  x_scales float32 [T][B][ceil(K / 128)] contiguous.
  *   w               e4m3 [R][K] contiguous;  w_scales float32 [ceil(R / 128)][ceil(K / 128)] contiguous.

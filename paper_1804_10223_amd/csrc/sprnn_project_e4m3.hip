@@ -281,8 +281,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(ProductArgs
 // and 64 scaled sums; the widened fragments and the running sums fill the registers (128 rows of w a wavefront are 27 too many).
 // Where a CU has one workgroup, one wavefront a SIMD would go through loads from LDS, products and sums one after the other:
 // KS = 2 gives a workgroup a second set of wavefronts and stages for every other slab, and the two sums meet in the end.
-// Measured on 8192 x 2304 x 9216: 365 us for outputs of any type (matrix instructions 139 us of it at 2.4 GHz; the chip runs at
-// 2.0 here).  Others came out within 5 % (eight wavefronts and three stages, half slabs in five stages), and widening once a
+// Measured on 8192 x 2304 x 9216: 365 to 385 us, by the card, for outputs of any type (matrix instructions 139 us of it at 2.4 GHz; the
+// chip runs at 1.7 to 1.9 here, and a profiler's single runs take up to 460).  Others came out within 5 % (eight wavefronts and three stages, half slabs in five stages), and widening once a
 // workgroup, on the way into LDS, a sixth slower: twice the bytes through LDS.
 constexpr int kWR = 2, kWM = 2, kIR = 2;           // wavefronts of a workgroup (and part) along w and x, 32 rows of w of each
 constexpr int kManyR = kWR * kIR * 32, kManyM = kWM * 64, kManyThreads = kWR * kWM * 64;

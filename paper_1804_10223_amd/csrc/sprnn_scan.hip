@@ -35,8 +35,8 @@ __device__ __forceinline__ void deal_by_length(const ScanArgs& a, int& column, i
 // the S lanes of a channel share out the steps of a tile, and hand d and d u over to their neighbours.  B and C of a tile
 // are the same for all channels and are brought into LDS in binary32 once a tile; the next tile's loads are in flight while
 // a tile is worked through, and two LDS buffers make one barrier a tile enough.  Bound by the vector units: for four states of
-// a lane and 16 steps 516 instructions and 72 exponentials, which take two turns each; they are busy 80 % of the time
-// (1 x 4096 x 2304 with 16 states: 55 us and 40 for the local run).
+// a lane and 16 steps 520 instructions and 72 exponentials, which take two turns each; they are busy three quarters of the time
+// (1 x 4096 x 2304 with 16 states: 60 us and 40 for the local run).
 // kLocal: a segment's effect only (H[segment + 1] from a zero state, the first from its true one; sums[segment] = sum of d).
 enum { kPlain, kKeeping, kLocal };     // what a run of the forward pass leaves: y; y and the states in front of every tile; its effect
 

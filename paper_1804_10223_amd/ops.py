@@ -4,10 +4,10 @@ The names mirror the second half of ``include/sprnn.h``; like ``binding`` this m
 and every call enqueues HIP kernels on torch's current stream of the tensors' device.  Activations are float32, float16
 or bfloat16 CUDA tensors whose last dimension is contiguous (the first two may have any strides: batch-major tensors and a
 range of the channels of a wider tensor need no copy); parameters and states are contiguous float32 tensors.  Outputs
-that the caller does not pass are allocated here, contiguous.  ``lengths`` (int32 [B], on the device) ends samples early:
-inputs behind a sample's end are not used, outputs there are zero.  Nothing here takes part in autograd: the backward
-passes are calls of their own, like those of ``SparseRNN``, and a call on tensors that require gradients warns that its
-results have none (not under ``torch.no_grad``).
+that the caller does not pass are allocated here, contiguous; those that are passed must not overlap inputs unless said
+otherwise.  ``lengths`` (int32 [B], on the device) ends samples early: inputs behind a sample's end are not used, outputs
+there are zero.  Nothing here takes part in autograd: the backward passes are calls of their own, like those of
+``SparseRNN``, and a call on tensors that require gradients warns that its results have none (not under ``torch.no_grad``).
 """
 from __future__ import annotations
 
