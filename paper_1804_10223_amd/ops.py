@@ -143,7 +143,7 @@ def _workspace(size, device):
 
 
 def _leads(t):
-    return t is not None and t.requires_grad
+    return getattr(t, "requires_grad", False)         # (what is no tensor is refused by name later)
 
 
 def _warn(what, level=3):
@@ -173,7 +173,9 @@ def scan_sizes(steps, batch, channels, states, groups=1):
 
 def _scan(index, u, dt, A, B, C, D, z, dt_bias, softplus, lengths):
     """sprnn_scan_t and the sizes (T, batch, C, N, groups)."""
-    if u.dim() != 3 or B is None or B.dim() != 4:
+    if not isinstance(B, torch.Tensor):
+        raise TypeError("B must be a tensor on cuda:%d" % index)
+    if u.dim() != 3 or B.dim() != 4:
         raise ValueError("u must be [T, B, C] and B must be [T, B, groups, N]")
     dtype = u.dtype
     wide, low = u.shape, B.shape
@@ -245,7 +247,9 @@ def selective_scan_backward(dy, u, dt, A, B, C, kept, D=None, z=None, dt_bias=No
 
 def _conv(index, x, weight, bias, silu, state, lengths):
     """sprnn_conv_t and the sizes (T, batch, C, K)."""
-    if x.dim() != 3 or weight is None or weight.dim() != 2:
+    if not isinstance(weight, torch.Tensor):
+        raise TypeError("weight must be a tensor on cuda:%d" % index)
+    if x.dim() != 3 or weight.dim() != 2:
         raise ValueError("x must be [T, B, C] and weight must be [C, K]")
     T, batch, channels = x.shape
     width = weight.shape[1]
@@ -306,7 +310,7 @@ def _norm_forward(x, weight, eps, residual, residual_out, y, scales, quantized):
     if x.dim() != 3:
         raise ValueError("x must be [T, B, W]")
     shape, dtype, device = x.shape, x.dtype, x.device
-    stream_dtype = dtype if residual is None else residual.dtype
+    stream_dtype = dtype if residual is None else getattr(residual, "dtype", None)
     norm = _norm(index, shape, dtype, stream_dtype, eps, weight)
     if torch.is_grad_enabled() and (x.requires_grad or _leads(weight) or _leads(residual)):
         _warn("rms_norm_fp8" if quantized else "rms_norm", 4)

@@ -345,3 +345,20 @@ def test_calls_on_tensors_that_require_gradients_say_that_there_are_none():
         ops.causal_conv(x, A)
         ops.rms_norm(x, eight)
         ops.project_fp8(q, one, q[:, 0], one[0])
+
+
+def test_arguments_that_are_no_tensors_are_refused_by_name():
+    ops = _ops()
+    x, A = torch.zeros((2, 1, 8), device="cuda"), torch.zeros((8, 4), device="cuda")
+    low, one = torch.zeros((2, 1, 1, 4), device="cuda"), torch.ones((2, 1, 1), device="cuda")
+    q = torch.zeros((2, 1, 8), dtype=torch.float8_e4m3fn, device="cuda")
+    for name, call in (("state", lambda v: ops.selective_scan(x, x, A, low, low, state=v)), ("D", lambda v: ops.selective_scan(x, x, A, low, low, D=v)),
+                       ("z", lambda v: ops.selective_scan(x, x, A, low, low, z=v)), ("state", lambda v: ops.causal_conv(x, A, state=v)),
+                       ("B", lambda v: ops.selective_scan(x, x, A, v, low)), ("C", lambda v: ops.selective_scan(x, x, A, low, v)),
+                       ("dt", lambda v: ops.selective_scan(x, v, A, low, low)), ("weight", lambda v: ops.causal_conv(x, v)),
+                       ("residual", lambda v: ops.rms_norm(x, residual=v)), ("d_residual", lambda v: ops.rms_norm_backward(x, x, d_residual=v)),
+                       ("bias", lambda v: ops.causal_conv(x, A, bias=v)), ("weight", lambda v: ops.rms_norm(x, v)),
+                       ("bias", lambda v: ops.project_fp8(q, one, q[:, 0], one[0], bias=v))):
+        for wrong in ([0.0] * 8, 1.0, x.cpu().numpy()):
+            with pytest.raises(TypeError, match=name):
+                call(wrong)
